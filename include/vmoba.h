@@ -257,6 +257,147 @@ int vmoba_attn_bwd(int B, int Hh, int64_t S, int D, int32_t n_blocks, const int3
                    const int32_t* rows, const int32_t* key_rows, const int32_t* kv_rows, void* workspace,
                    size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * What stands around the sparse layer: queries and keys are normalised (vmoba_rmsnorm_fwd) and turned by their positions on the
+ * latent grid (vmoba_rope) before it, and the layers and sampling steps that stay dense take vmoba_dense_fwd in its place.  The
+ * conventions above hold for these calls, too, unless a call says otherwise.
+ */
+
+/* A row's rotated channels are its first R = dims[0] + ... + dims[n_axes - 1]; pair p (0 <= p < R/2) is turned by
+ * frequency[p] * position along the pair's axis: the first dims[0]/2 pairs belong to axis 0, the next dims[1]/2 to axis 1, ... */
+typedef enum {
+    VMOBA_ROPE_HALF = 0,       /* pair p = channels p and p + R/2     */
+    VMOBA_ROPE_INTERLEAVED = 1 /* pair p = channels 2p and 2p + 1     */
+} vmoba_rope_layout;
+
+/* How frequencies are scaled for sequences longer than those of training, by `factor` >= 1 (Su et al., arXiv 2104.09864;
+ * position interpolation, arXiv 2306.15595; YaRN, arXiv 2309.00071).  An axis of d channels has the frequencies
+ * w_i = base^(-2i/d), i = 0 .. d/2 - 1, and
+ *   PLAIN   w_i                     LINEAR  w_i / factor               NTK  the same with base * factor^(d/(d-2)) (d > 2)
+ *   YARN    (1 - g) w_i / factor + g w_i, g = clamp((train_len w_i / 2 pi - 1) / 31, 0, 1); rotated values are also multiplied
+ *           by 0.1 ln(factor) + 1 */
+typedef enum { VMOBA_ROPE_PLAIN = 0, VMOBA_ROPE_LINEAR = 1, VMOBA_ROPE_NTK = 2, VMOBA_ROPE_YARN = 3 } vmoba_rope_scaling;
+
+/* Host helper: the R/2 frequencies in radians per position into `freqs` (host), the factor of the rotated values into *mscale (host).
+ * dims: 1 to 3 positive even numbers; train_len is read by YARN only. */
+int vmoba_rope_freqs(int n_axes, const int32_t* dims, double base, int scaling, double factor, int64_t train_len, double* freqs,
+                     float* mscale);
+
+/*
+ * vmoba_rope -- rotary positions, on n_tensors tensors at once (queries and keys):
+ *   u = mscale (a cos x - b sin x),  v = mscale (a sin x + b cos x)   for the pair (a, b) and its angle x = frequency * position;
+ * channels from R on are copied.  inverse = 1 turns by -x with the same mscale, which is the gradient of the call with inverse = 0.
+ *
+ *  Hh         host array of n_tensors head counts (shared key heads: fewer than the queries')
+ *  in / out   host arrays of n_tensors descriptors (1..8), (b, s, h, d) with D channels, all of one dtype; out[i] may be in[i] (same
+ *             strides); it may not overlap any input otherwise
+ *  freqs      [R/2] float64 (device)
+ *  positions  optional int32 [B or 1][S][n_axes]: position of token s along each axis; pos_stride_b elements from one batch element
+ *             to the next (0: shared).  Null: with n_axes = 3 the coordinates of token s on grid->T x H x W (S = T*H*W), with n_axes = 1
+ *             (grid is not read) s itself
+ *  first      added to the position along axis 0 (the first token's position in a longer sequence)
+ *  D is even, 2 <= D <= 1024, R <= D.  Angles are reduced in float64, so far positions lose nothing; products are float32, rounded once.
+ *  S = 0 or B = 0 is a call that does nothing.
+ */
+int vmoba_rope(int B, int64_t S, int D, int n_tensors, const int32_t* Hh, const vmoba_tensor* in, const vmoba_tensor* out,
+               const double* freqs, int n_axes, const int32_t* dims, int layout, int inverse, float mscale, const vmoba_grid* grid,
+               int64_t first, const int32_t* positions, int64_t pos_stride_b, void* stream);
+
+/* An 8-bit type for the output of vmoba_rmsnorm_fwd alone (OCP e4m3: largest value 448, no infinities).  Not a vmoba_dtype of
+ * any other call. */
+#define VMOBA_F8E4M3 2
+
+/* Bytes of workspace vmoba_rmsnorm_bwd needs when it computes dweight. */
+size_t vmoba_rmsnorm_workspace_bytes(int B, int Hh, int64_t S, int D);
+
+/*
+ * vmoba_rmsnorm_fwd -- root-mean-square norm over the D channels of every (b, s, h), after adding a residual:
+ *   t = x + residual, rounded to the tensors' dtype (x alone without a residual);  inv = 1 / sqrt(mean(t^2) + eps);  y = t * inv * weight
+ * (to normalise over all heads of a token, describe it as one head of Hh * D channels).
+ *
+ *  x, residual  float32 or bfloat16, one dtype; residual may be null
+ *  total        t, the same dtype; needed with a residual, null without
+ *  weight       [D], weight_dtype float32 or bfloat16; null: ones
+ *  y            the same dtype, or VMOBA_F8E4M3 with y_scale: then y holds round(t * inv * weight / y_scale), y_scale = the row's largest
+ *               magnitude / 448 (1 for a row of zeros).  The quotient is taken in float32 and rounded once, to nearest even
+ *  y_scale      float32 [B, S, Hh], with VMOBA_F8E4M3 alone
+ *  inv_rms      optional float32 [B, S, Hh]: inv, which the backward call reads
+ *  Any strides and element-aligned addresses with contiguous channels; 1 <= D <= 16384.  An output may lie exactly on an input (same address
+ *  and strides, same dtype).  Sums are float32.  A row that holds a NaN or an infinity gives NaNs (and zeros) in that row alone.
+ *  S = 0 or B = 0 is a call that does nothing.
+ */
+int vmoba_rmsnorm_fwd(int B, int Hh, int64_t S, int D, const vmoba_tensor* x, const vmoba_tensor* residual, const void* weight,
+                      int weight_dtype, float eps, const vmoba_tensor* total, const vmoba_tensor* y, float* y_scale, float* inv_rms,
+                      void* stream);
+
+/*
+ * vmoba_rmsnorm_bwd -- its gradient.  x is what was normalised (t), inv_rms what the forward call wrote.  With n = t * inv, g = dy * weight:
+ *   dx = inv (g - n mean(g n)) + dtotal,    dweight = sum over all rows of dy * n
+ *  dy, dx   of x's dtype;  dtotal optional: the gradient that reaches t by itself (dx is the gradient of x and of the residual)
+ *  dweight  optional float32 [D], written; needs the workspace.  Summed in a fixed order: the same call gives the same bits
+ *  dx may lie exactly on dy, dtotal or x.  S = 0 or B = 0: dweight is zero.
+ */
+int vmoba_rmsnorm_bwd(int B, int Hh, int64_t S, int D, const vmoba_tensor* x, const void* weight, int weight_dtype, const float* inv_rms,
+                      const vmoba_tensor* dy, const vmoba_tensor* dtotal, const vmoba_tensor* dx, float* dweight, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/*
+ * vmoba_key_ranges -- the keys that each query of a dense call may read, as one range: lo <= key < hi.  Query r of batch element b stands at
+ * position p = q_pos[b][r], or q_first + r without q_pos; key j at position j.
+ *  doc_off  optional int32 [B or 1][n_docs + 1], ascending: documents lie at positions doc_off[d] <= p < doc_off[d + 1], and a query
+ *           reads its own document only; one outside every document gets an empty range (lo = hi = 0).  doc_stride_b elements from one batch
+ *           element to the next (0: shared).  Null: one document of all Sk positions (n_docs = 1), which every query is inside.
+ *           A batch of padded sequences is one document {0, length} each
+ *  prefix   optional int32 [B or 1][n_docs]: with causal, the first prefix[d] positions of document d are seen by all its queries;
+ *           prefix_stride_b as above
+ *  causal   0 or 1: a query sees no key behind its own position, the prefix excepted
+ *  lo, hi   int32 [B][Sq], written; 0 <= lo <= hi <= Sk whatever the arrays hold
+ */
+int vmoba_key_ranges(int B, int64_t Sq, int64_t Sk, const int32_t* doc_off, int64_t doc_stride_b, int32_t n_docs, const int32_t* prefix,
+                     int64_t prefix_stride_b, int causal, const int32_t* q_pos, int64_t q_first, int32_t* lo, int32_t* hi, void* stream);
+
+/* How scores of a dense call are formed.  s = z = softmax_scale * <q, k>; with cap > 0: s = cap * tanh(z / cap); with slopes:
+ * s - slopes[h] * |p - j| for query head h, query position p and key position j (positions as in vmoba_key_ranges). */
+typedef struct {
+    float softmax_scale;     /* finite */
+    float cap;               /* 0: none; otherwise positive and finite */
+    const float* slopes;     /* device float32 [Hq], finite, or null: constants, they get no gradient */
+    const int32_t* key_lo;   /* device int32 [B][Sq], both or neither: query r reads keys lo <= j < hi (clamped to 0 .. Sk); */
+    const int32_t* key_hi;   /* lo >= hi: none.  Null: every query reads every key.  Any ranges, not only those of vmoba_key_ranges */
+    const int32_t* q_pos;    /* device int32 [B][Sq] or null: positions of the queries, between -2^30 and 2^30 (slopes alone read them) */
+    int64_t q_first;         /* without q_pos query r stands at q_first + r */
+} vmoba_scores;
+
+/* Bytes of workspace of vmoba_dense_fwd (op = VMOBA_OP_ATTN_FWD) and vmoba_dense_bwd (VMOBA_OP_ATTN_BWD); 0: not supported. */
+size_t vmoba_dense_workspace_bytes(int op, int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, int dtype);
+
+/*
+ * vmoba_dense_fwd -- attention of every query to all keys of its range.  O(q) = sum_j softmax_j(s_j) V(j), LSE [B, Hq, Sq] float32 the
+ * natural-log-sum-exp of the scores; a query without keys gets O = 0 and LSE = -inf.  Query head h reads key head h / (Hq / Hkv).
+ *  Q, O  (b, s, h, d) of Sq tokens and Hq heads;  K, V  of Sk tokens and Hkv heads (Hq a multiple of Hkv).  One dtype, D in {64, 128}.
+ *  Sq, Sk from 1 on (one query against a long cache is split over its keys); Sq * Hq / Hkv and Sk below 2^24.
+ *  Rows outside a query's range never reach its results, whatever they hold (NaN and infinities included).
+ *  Sums and the soft-max are float32; bfloat16 inputs are multiplied on the matrix cores, weights rounded to bfloat16 for the second
+ *  product; float32 inputs are multiplied in float32.
+ *  Limit: a row stride of K and V of at least 0 and below 2^23 bytes, and Sk rows of it below 4 GiB; otherwise VMOBA_ERR_UNSUPPORTED.
+ */
+int vmoba_dense_fwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_tensor* Q, const vmoba_tensor* K,
+                    const vmoba_tensor* V, const vmoba_scores* how, const vmoba_tensor* O, float* LSE, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/*
+ * vmoba_dense_bwd -- its gradient: delta = rowsum(dO * O), dV = A^T dO, dz = A * (dO V^T - delta) * (1 - (s_capped / cap)^2),
+ * dQ = softmax_scale * dz K, dK = softmax_scale * dz^T Q, summed over the query heads that share a key head.  The same call gives the
+ * same bits.  O and LSE are the forward results; dQ, dK, dV are written, queries and keys without a pair get zeros.
+ *  A query whose row of Q, O or dO holds a NaN or an infinity gives NaNs in its row of dQ and in the rows of dK and dV of the keys it reads,
+ *  and in no others.
+ *  Limits as in the forward call.
+ */
+int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_tensor* Q, const vmoba_tensor* K,
+                    const vmoba_tensor* V, const vmoba_scores* how, const vmoba_tensor* O, const float* LSE, const vmoba_tensor* dO,
+                    const vmoba_tensor* dQ, const vmoba_tensor* dK, const vmoba_tensor* dV, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
 /*
  * vmoba_profile_events -- measurement aid, not part of the method.  Asks the library to record
  * the caller's two hipEvent_t (passed as void*) on the call's stream immediately before and after

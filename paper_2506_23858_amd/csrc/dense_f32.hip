@@ -1,0 +1,422 @@
+// Dense attention, float32: the same decomposition as the bfloat16 kernels on v_mfma_f32_32x32x2_f32, products in full float32.
+//
+// Operand plumbing (lane = 32 * hf + l32): A: row l32, k = hf; B: column l32, k = hf; C/D: column l32, rows 8 * i + 4 * hf + r as value
+// 4 * i + r.  The order of a contraction is free, so
+//   * over channels, lane half hf takes channels hf * D/2 + t at step t: both operands are runs of a row, 16 bytes at a time;
+//   * over 32 keys (or rows), step 4 * i + r takes keys 8 * i + 4 * hf + r: the accumulator value itself is the B operand, and A is a
+//     column of the tile, 32 consecutive floats of two rows.
+// Tiles of 32 rows go through registers to LDS, requested one tile ahead, in rows padded by 16 bytes.  One such instruction is 64 cycles of the
+// matrix pipe for one LDS read of 4 or a quarter of one of 16 bytes: the pipe is what bounds these kernels.
+#include "dense_common.h"
+
+#include <cfloat>
+#include <cmath>
+
+namespace {
+
+template <int D> constexpr int PITCH = D + 4;                // floats per tile row
+
+// 32 rows of a tensor through registers to LDS, by NT threads.
+template <int D, int NT>
+struct Stage {
+    static constexpr int PPR = D / 4, N = 32 * PPR / NT;
+    f32x4_t x[N];
+    template <class F>
+    __device__ __forceinline__ void load(F row) {            // row(r): pointer to row r of the tile
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = i * NT + (int)threadIdx.x;
+            x[i] = *reinterpret_cast<const f32x4_t*>(row(p / PPR) + p % PPR * 16);
+        }
+    }
+    __device__ __forceinline__ void store(float* tile) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = i * NT + (int)threadIdx.x;
+            *reinterpret_cast<f32x4_t*>(tile + p / PPR * PITCH<D> + p % PPR * 4) = x[i];
+        }
+    }
+};
+// acc += A . B over the channels: A rows l32 of an LDS tile, B the lane's fragment (channels hf * D/2 ...).
+template <int D>
+__device__ __forceinline__ f32x16_t over_channels(const float* tile, const float (&frag)[D / 2], f32x16_t acc, int l32, int hf) {
+    const float* row = tile + l32 * PITCH<D> + hf * (D / 2);
+#pragma unroll
+    for (int t = 0; t < D / 2; t += 4) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(row + t);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], frag[t + j], acc, 0, 0, 0);
+    }
+    return acc;
+}
+// acc[dt] += (tile columns 32 * dt + l32)^T . p over the tile's 32 rows; CLEAN: values that are not finite count as 0.
+template <int D>
+__device__ __forceinline__ void over_rows(const float* tile, const f32x16_t& p, f32x16_t (&acc)[D / 32], int l32, int hf, bool clean, unsigned& found) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const float* row = tile + (8 * (v >> 2) + 4 * hf + (v & 3)) * PITCH<D> + l32;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            float x = row[32 * dt];
+            if (clean && !(fabsf(x) < INFINITY)) {
+                x = 0.f;
+                found = 1u;
+            }
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[v], acc[dt], 0, 0, 0);
+        }
+    }
+}
+template <int D>
+__device__ __forceinline__ void load_fragment(float (&f)[D / 2], const char* row, int hf) {
+#pragma unroll
+    for (int t = 0; t < D / 2; t += 4) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(row + (hf * (D / 2) + t) * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[t + j] = x[j];
+    }
+}
+// A wavefront's 32 x D result from accumulators (column l32 = row of the result) to rows: 16-byte stores.
+template <int D>
+__device__ __forceinline__ void store_row(char* row, const f32x16_t (&acc)[D / 32], float f, int hf) {
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4_t x = {acc[dt][4 * i] * f, acc[dt][4 * i + 1] * f, acc[dt][4 * i + 2] * f, acc[dt][4 * i + 3] * f};
+            *reinterpret_cast<f32x4_t*>(row + (32 * dt + 8 * i + 4 * hf) * 4) = x;
+        }
+}
+// Base-2 score of x = <q, k> before the bias (scl: signed scale * log2 e); t: tanh of the capped score.
+template <bool CAP>
+__device__ __forceinline__ float score32(const DenseArgs& a, float x, float scl, float& t) {
+    if constexpr (CAP) {
+        t = tanhf((a.negate ? -x : x) * a.cap_arg);
+        return a.cap2 * t;
+    } else {
+        return x * scl;
+    }
+}
+const f32x16_t zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+struct Keys { int any_lo, any_hi, all_lo, all_hi; };
+// Keys that any row of the workgroup reads, and that all rows of the wavefront read (no row without keys among them); w: 2 * NW words of LDS.
+template <int NW>
+__device__ __forceinline__ Keys tile_keys(int lo, int hi, int wave, int lane, int* w) {
+    const bool some = lo < hi;
+    Keys k = {some ? lo : INT32_MAX, some ? hi : 0, some ? lo : INT32_MAX, some ? hi : 0};
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+        k.any_lo = min(k.any_lo, __shfl_xor(k.any_lo, o, 64));
+        k.any_hi = max(k.any_hi, __shfl_xor(k.any_hi, o, 64));
+        k.all_lo = max(k.all_lo, __shfl_xor(k.all_lo, o, 64));
+        k.all_hi = min(k.all_hi, __shfl_xor(k.all_hi, o, 64));
+    }
+    if constexpr (NW > 1) {
+        if (lane == 0) {
+            w[wave] = k.any_lo;
+            w[NW + wave] = k.any_hi;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            k.any_lo = min(k.any_lo, w[i]);
+            k.any_hi = max(k.any_hi, w[NW + i]);
+        }
+    }
+    k.any_lo = __builtin_amdgcn_readfirstlane(k.any_lo);
+    k.any_hi = __builtin_amdgcn_readfirstlane(k.any_hi);
+    k.all_lo = __builtin_amdgcn_readfirstlane(k.all_lo);
+    k.all_hi = __builtin_amdgcn_readfirstlane(k.all_hi);
+    if (k.any_lo >= k.any_hi) k.any_lo = k.any_hi = 0;
+    return k;
+}
+
+template <int D, int NW, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) {
+    constexpr int NT = 64 * NW, TILE = 32 * PITCH<D>;
+    __shared__ __align__(16) float smem[2 * TILE];
+    __shared__ int words[2 * NW];
+    const int tiles = (a.M + 32 * NW - 1) / (32 * NW);
+    const int item = dense_item(a.B * a.Hkv * tiles * a.splits);
+    if (item < 0) return;
+    const int split = item % a.splits, tile = item / a.splits % tiles, bh = item / a.splits / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
+    const int m0 = tile * 32 * NW + wave * 32, m = m0 + l32, mc = min(m, a.M - 1), q = mc / a.G, h = hk * a.G + (mc - q * a.G);
+    const float scl = a.negate ? -a.scale_log2 : a.scale_log2;
+    const int2 range = dense_range(a, b, q);
+    const int lo = m < a.M ? range.x : 0, hi = m < a.M ? range.y : 0;
+    const float slope2 = BIAS ? a.slopes[h] * DENSE_LOG2E : 0.f;
+    const int pos = BIAS ? dense_position(a, b, q) : 0;
+    const Keys keys = tile_keys<NW>(lo, hi, wave, lane, words);
+    int k_first = keys.any_lo, k_end = keys.any_hi;
+    if (a.splits > 1) {
+        const int groups = (k_end - k_first + 31) / 32, per = (groups + a.splits - 1) / a.splits;
+        const int s0 = min(split * per, groups), s1 = min(s0 + per, groups);
+        k_end = min(k_end, k_first + s1 * 32);
+        k_first += s0 * 32;
+    }
+    float qf[D / 2];
+    load_fragment<D>(qf, row_ptr(a.Q, b, q, h, 4), hf);
+    f32x16_t acc[D / 32];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16;
+    float m_run = -3e38f, l_run = 0.f;
+    unsigned found = 0;
+    const char *kbase = row_ptr(a.K, b, 0, hk, 4), *vbase = row_ptr(a.V, b, 0, hk, 4);
+    const long long kss = a.K.stride_s * 4, vss = a.V.stride_s * 4;
+    Stage<D, NT> sk, sv;
+    auto fetch = [&](int kb) {
+        sk.load([&](int r) { return kbase + min(kb + r, a.Sk - 1) * kss; });
+        sv.load([&](int r) { return vbase + min(kb + r, a.Sk - 1) * vss; });
+    };
+    if (k_first < k_end) fetch(k_first);
+    for (int kb = k_first; kb < k_end; kb += 32) {
+        __syncthreads();
+        sk.store(smem);
+        sv.store(smem + TILE);
+        __syncthreads();
+        if (kb + 32 < k_end) fetch(kb + 32);
+        const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi || kb + 32 > k_end;
+        f32x16_t s = over_channels<D>(smem, qf, zero16, l32, hf);
+        const float rel = BIAS ? (float)(pos - kb - 4 * hf) : 0.f;
+        const int first_key = lo - kb - 4 * hf, end = min(hi, k_end) - kb - 4 * hf;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int key = 8 * (v >> 2) + (v & 3);
+            float t, s2 = score32<CAP>(a, s[v], scl, t);
+            if constexpr (BIAS) s2 = fmaf(-slope2, fabsf(rel - (float)key), s2);
+            if constexpr (CAP || BIAS) s[v] = s2;
+            if (!masked || (key >= first_key && key < end)) mx = fmaxf(mx, s2);
+        }
+        mx = swap_halves_max(mx);
+        const float m_new = fmaxf(m_run, mx), alpha = exp2_raw(m_run - m_new);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int key = 8 * (v >> 2) + (v & 3);
+            float p = exp2_raw(CAP || BIAS ? s[v] - m_run : fmaf(s[v], scl, -m_run));
+            if (masked && (key < first_key || key >= end)) p = 0.f;
+            l_run += p;
+            s[v] = p;
+        }
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[dt][v] *= alpha;
+        }
+        over_rows<D>(smem + TILE, s, acc, l32, hf, masked, found);
+    }
+    const float l = swap_halves_sum(l_run), inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m_run + log2f(l);
+    const long long part0 = ((long long)split * a.B * a.Hkv + bh) * a.M;
+    if (m < a.M) {
+        if (a.splits > 1) {
+            store_row<D>((char*)(a.part_o + (part0 + m) * D), acc, inv, hf);
+            if (hf == 0) a.part_lse[part0 + m] = lse2;
+        } else {
+            store_row<D>(const_cast<char*>(row_ptr(a.O, b, q, h, 4)), acc, inv, hf);
+            if (hf == 0) a.LSE[((long long)b * a.Hq + h) * a.Sq + q] = lse2 * DENSE_LN2;
+        }
+    }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(found != 0) == 0, 1)) return;
+    // (rows m0 + 16 + lane % 16 are lanes 16 .. 31)
+    dense_repair<float, D, CAP, BIAS>(a, b, hk, m0, lane, part0, k_first, k_end, keys.all_lo, keys.all_hi, lo, __shfl(lo, 16 + (lane & 15), 64), hi,
+                                      __shfl(hi, 16 + (lane & 15), 64), lse2, __shfl(lse2, 16 + (lane & 15), 64));
+}
+
+// P and dz of one pair from x = <q, k> and dp = dP - delta.
+template <bool CAP>
+__device__ __forceinline__ void pair_gradient(const DenseArgs& a, float x, float scl, float bias2, float lse2, float dp, float& p, float& dz) {
+    float t = 0.f;
+    const float s2 = score32<CAP>(a, x, scl, t);
+    p = exp2_raw(CAP ? s2 - bias2 - lse2 : fmaf(x, scl, -bias2 - lse2));
+    dz = p * dp * (CAP ? 1.f - t * t : 1.f);
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
+    constexpr int TILE = 32 * PITCH<D>;
+    __shared__ __align__(16) float smem[2 * TILE];
+    __shared__ int words[8];
+    const int tiles = (a.M + 127) / 128;
+    const int item = dense_item(a.B * a.Hkv * tiles);
+    if (item < 0) return;
+    const int tile = item % tiles, bh = item / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
+    const int m = tile * 128 + wave * 32 + l32, mc = min(m, a.M - 1), q = mc / a.G, h = hk * a.G + (mc - q * a.G);
+    const float scl = a.negate ? -a.scale_log2 : a.scale_log2;
+    const RowInfo& info = (reinterpret_cast<const RowInfo*>(a.row_info) + (long long)bh * ((a.M + 31) / 32))[mc >> 5];
+    const int lo = m < a.M ? info.lo[mc & 31] : 0, hi = m < a.M ? info.hi[mc & 31] : 0;
+    const float lse2 = info.lse2[mc & 31], nd = info.ndelta[mc & 31], slope2 = BIAS ? info.slope2[mc & 31] : 0.f;
+    const int pos = BIAS ? info.pos[mc & 31] : 0;
+    const Keys keys = tile_keys<4>(lo, hi, wave, lane, words);
+    float qf[D / 2], dof[D / 2];
+    load_fragment<D>(qf, row_ptr(a.Q, b, q, h, 4), hf);
+    load_fragment<D>(dof, row_ptr(a.dO, b, q, h, 4), hf);
+    f32x16_t acc[D / 32];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16;
+    unsigned found = 0;
+    const char *kbase = row_ptr(a.K, b, 0, hk, 4), *vbase = row_ptr(a.V, b, 0, hk, 4);
+    const long long kss = a.K.stride_s * 4, vss = a.V.stride_s * 4;
+    Stage<D, 256> sk, sv;
+    auto fetch = [&](int kb) {
+        sk.load([&](int r) { return kbase + min(kb + r, a.Sk - 1) * kss; });
+        sv.load([&](int r) { return vbase + min(kb + r, a.Sk - 1) * vss; });
+    };
+    if (keys.any_lo < keys.any_hi) fetch(keys.any_lo);
+    for (int kb = keys.any_lo; kb < keys.any_hi; kb += 32) {
+        __syncthreads();
+        sk.store(smem);
+        sv.store(smem + TILE);
+        __syncthreads();
+        if (kb + 32 < keys.any_hi) fetch(kb + 32);
+        const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi;
+        f32x16_t s = over_channels<D>(smem, qf, zero16, l32, hf), dp;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dp[v] = nd;
+        dp = over_channels<D>(smem + TILE, dof, dp, l32, hf);
+        const float rel = BIAS ? (float)(pos - kb - 4 * hf) : 0.f;
+        const int first_key = lo - kb - 4 * hf, end = hi - kb - 4 * hf;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int key = 8 * (v >> 2) + (v & 3);
+            float p, dz;
+            pair_gradient<CAP>(a, s[v], scl, BIAS ? slope2 * fabsf(rel - (float)key) : 0.f, lse2, dp[v], p, dz);
+            s[v] = masked && (key < first_key || key >= end) ? 0.f : dz;
+        }
+        over_rows<D>(smem, s, acc, l32, hf, masked, found);
+    }
+    if (m < a.M) store_row<D>(const_cast<char*>(row_ptr(a.dQ, b, q, h, 4)), acc, a.scale, hf);
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
+    constexpr int TILE = 32 * PITCH<D>;
+    __shared__ __align__(16) float smem[2 * TILE];
+    __shared__ RowInfo ri;
+    const int tiles = (a.Sk + 127) / 128;
+    const int item = dense_item(a.B * a.Hkv * tiles);
+    if (item < 0) return;
+    const int tile = item % tiles, bh = item / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
+    const int k0 = tile * 128, kw = k0 + wave * 32, key = kw + l32;
+    const float scl = a.negate ? -a.scale_log2 : a.scale_log2;
+    const int n_chunks = (a.M + 31) / 32;
+    const RowInfo* info = reinterpret_cast<const RowInfo*>(a.row_info) + (long long)bh * n_chunks;
+    const int4* bounds = a.row_bounds + (long long)bh * n_chunks;
+    float kf[D / 2], vf[D / 2];
+    load_fragment<D>(kf, row_ptr(a.K, b, min(key, a.Sk - 1), hk, 4), hf);
+    load_fragment<D>(vf, row_ptr(a.V, b, min(key, a.Sk - 1), hk, 4), hf);
+    f32x16_t dk[D / 32], dv[D / 32];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zero16;
+    unsigned found = 0;
+    Stage<D, 256> sq, so;
+    uint32_t si = 0;                                         // the thread's word of the row information
+    int window = 0;
+    unsigned long long pending = 0;
+    auto look = [&]() {
+        const int c = window + lane;
+        const int4 r = c < n_chunks ? bounds[c] : make_int4(INT32_MAX, 0, 0, 0);
+        pending = __builtin_amdgcn_ballot_w64(r.x < k0 + 128 && r.y > k0);
+    };
+    auto next_chunk = [&]() {
+        while (pending == 0) {
+            window += 64;
+            if (window >= n_chunks) return -1;
+            look();
+        }
+        const int i = __builtin_ctzll(pending);
+        pending &= pending - 1;
+        return window + i;
+    };
+    auto fetch = [&](int c) {
+        auto row = [&](const TensorView& t) {
+            return [&, c](int r) {
+                const int m = min(c * 32 + r, a.M - 1), q = m / a.G;
+                return row_ptr(t, b, q, hk * a.G + (m - q * a.G), 4);
+            };
+        };
+        sq.load(row(a.Q));
+        so.load(row(a.dO));
+        si = reinterpret_cast<const uint32_t*>(info + c)[tid];
+    };
+    look();
+    int c = next_chunk();
+    if (c >= 0) fetch(c);
+    while (c >= 0) {
+        const int4 bd = bounds[c];
+        __syncthreads();
+        sq.store(smem);
+        so.store(smem + TILE);
+        reinterpret_cast<uint32_t*>(&ri)[tid] = si;
+        __syncthreads();
+        c = next_chunk();
+        if (c >= 0) fetch(c);
+        const int all_lo = __builtin_amdgcn_readfirstlane(bd.z), all_hi = __builtin_amdgcn_readfirstlane(bd.w);
+        const bool masked = kw < all_lo || kw + 32 > all_hi;
+        f32x16_t s = over_channels<D>(smem, kf, zero16, l32, hf), dp;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dp[v] = ri.ndelta[8 * (v >> 2) + 4 * hf + (v & 3)];
+        dp = over_channels<D>(smem + TILE, vf, dp, l32, hf);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int r = 8 * (v >> 2) + 4 * hf + (v & 3);
+            float p, dz;
+            pair_gradient<CAP>(a, s[v], scl, BIAS ? ri.slope2[r] * fabsf((float)(ri.pos[r] - key)) : 0.f, ri.lse2[r], dp[v], p, dz);
+            if (masked) {
+                const bool reads = key >= ri.lo[r] && key < ri.hi[r];
+                // (a row of dO that is not finite shows in delta; its values are taken out of the product below)
+                p = !reads ? 0.f : fabsf(ri.ndelta[r]) < INFINITY ? p : NAN;
+                dz = reads ? dz : 0.f;
+            }
+            s[v] = p;
+            dp[v] = dz;
+        }
+        over_rows<D>(smem + TILE, s, dv, l32, hf, masked, found);
+        over_rows<D>(smem, dp, dk, l32, hf, masked, found);
+    }
+    if (key < a.Sk) {
+        store_row<D>(const_cast<char*>(row_ptr(a.dK, b, key, hk, 4)), dk, a.scale, hf);
+        store_row<D>(const_cast<char*>(row_ptr(a.dV, b, key, hk, 4)), dv, 1.f, hf);
+    }
+}
+
+#define BY_SCORES(LAUNCH)                   \
+    do {                                    \
+        if (cap && a.slopes) LAUNCH(true, true);   \
+        else if (cap) LAUNCH(true, false);         \
+        else if (a.slopes) LAUNCH(false, true);    \
+        else LAUNCH(false, false);                 \
+    } while (0)
+
+template <int D, int NW>
+void launch_fwd(bool cap, hipStream_t st, const DenseArgs& a) {
+    const dim3 grid(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.M, 32 * NW) * a.splits)), block(64 * NW);
+#define LAUNCH(CAP, BIAS) dense_fwd_f32_kernel<D, NW, CAP, BIAS><<<grid, block, 0, st>>>(a)
+    BY_SCORES(LAUNCH);
+#undef LAUNCH
+}
+template <int D>
+void launch_bwd(bool cap, hipStream_t st, const DenseArgs& a) {
+    const dim3 gq(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.M, 128))), gk(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.Sk, 128))), block(256);
+#define LAUNCH(CAP, BIAS)                                            \
+    do {                                                             \
+        dense_dq_f32_kernel<D, CAP, BIAS><<<gq, block, 0, st>>>(a);  \
+        dense_dkv_f32_kernel<D, CAP, BIAS><<<gk, block, 0, st>>>(a); \
+    } while (0)
+    BY_SCORES(LAUNCH);
+#undef LAUNCH
+}
+
+}  // namespace
+
+void launch_dense_fwd_f32(int D, bool cap, hipStream_t st, const DenseArgs& a) {
+    const bool few = a.M <= DENSE_FEW_ROWS;
+    if (D == 128) few ? launch_fwd<128, 1>(cap, st, a) : launch_fwd<128, 4>(cap, st, a);
+    else few ? launch_fwd<64, 1>(cap, st, a) : launch_fwd<64, 4>(cap, st, a);
+}
+void launch_dense_bwd_f32(int D, bool cap, hipStream_t st, const DenseArgs& a) { D == 128 ? launch_bwd<128>(cap, st, a) : launch_bwd<64>(cap, st, a); }
