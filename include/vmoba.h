@@ -391,7 +391,7 @@ int vmoba_dense_fwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const
  * same bits.  O and LSE are the forward results; dQ, dK, dV are written, queries and keys without a pair get zeros.
  *  A query whose row of Q, O or dO holds a NaN or an infinity gives NaNs in its row of dQ and in the rows of dK and dV of the keys it reads,
  *  and in no others.
- *  Limits as in the forward call.
+ *  Limits as in the forward call, for Q and dO (Sq rows) as well; with shared key heads their head strides are not negative.
  */
 int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_tensor* Q, const vmoba_tensor* K,
                     const vmoba_tensor* V, const vmoba_scores* how, const vmoba_tensor* O, const float* LSE, const vmoba_tensor* dO,

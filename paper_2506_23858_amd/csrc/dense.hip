@@ -46,23 +46,35 @@ __global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
     const long long n = (long long)a.B * a.Hkv * a.M, i = ((long long)blockIdx.x * 256 + threadIdx.x) / LPR;
     const int part = threadIdx.x % LPR;
     if (i >= n) return;
+    constexpr int MB = 8;                                    // splits in flight
     float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) {
-        const float l = a.part_lse[s * n + i];
-        top = l > top || l != l ? l : top;                   // (a NaN stays)
+    for (int s0 = 0; s0 < a.splits; s0 += MB) {
+        float l[MB];
+#pragma unroll
+        for (int u = 0; u < MB; ++u) l[u] = a.part_lse[min(s0 + u, a.splits - 1) * n + i];
+#pragma unroll
+        for (int u = 0; u < MB; ++u) top = l[u] > top || l[u] != l[u] ? l[u] : top;      // (a NaN stays)
     }
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
     float sum = 0.f;
-    if (top != -INFINITY)
-        for (int s = 0; s < a.splits; ++s) {
-            const float w = exp2_raw(a.part_lse[s * n + i] - top);
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(a.part_o + (s * n + i) * D + part * 4);
-            if (w == 0.f) continue;                          // a split without keys of this row
-            sum += w;
-            acc += x * w;
+    for (int s0 = 0; s0 < a.splits && top != -INFINITY; s0 += MB) {
+        float w[MB];
+        f32x4_t x[MB];
+#pragma unroll
+        for (int u = 0; u < MB; ++u) {
+            const long long at = min(s0 + u, a.splits - 1) * n + i;
+            w[u] = s0 + u < a.splits ? exp2_raw(a.part_lse[at] - top) : 0.f;
+            x[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + part * 4);
         }
+#pragma unroll
+        for (int u = 0; u < MB; ++u) {
+            if (w[u] == 0.f) continue;                       // a split without keys of this row
+            sum += w[u];
+            acc += x[u] * w[u];
+        }
+    }
     const float inv = top == -INFINITY ? 0.f : 1.f / sum;
-    const int bh = (int)(i / a.M), m = (int)(i - (long long)bh * a.M), b = bh / a.Hkv, hk = bh - b * a.Hkv, q = m / a.G, h = hk * a.G + (m - q * a.G);
+    const int bh = (int)(i / a.M), m = (int)(i - (long long)bh * a.M), b = bh / a.Hkv, hk = bh - b * a.Hkv, q = query_of(a, m), h = hk * a.G + (m - q * a.G);
     char* dst = const_cast<char*>(row_ptr(a.O, b, q, h, sizeof(T)));
     if constexpr (sizeof(T) == 2) {
         const u32x2_t v = {pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
@@ -73,13 +85,114 @@ __global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
     if (part == 0) a.LSE[((long long)b * a.Hq + h) * a.Sq + q] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * DENSE_LN2;
 }
 
+// Joins the splits of a backward call's dK and dV: sums in the order of the splits.
+template <class T, int D>
+__global__ __launch_bounds__(256) void dense_sum_kernel(DenseArgs a) {
+    constexpr int LPR = D / 4;
+    const long long n = (long long)a.B * a.Hkv * a.Sk, i = ((long long)blockIdx.x * 256 + threadIdx.x) / LPR;
+    const int part = threadIdx.x % LPR;
+    if (i >= 2 * n) return;
+    const long long row = i < n ? i : i - n;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) acc += *reinterpret_cast<const f32x4_t*>(a.part_o + (2 * s * n + i) * D + part * 4);
+    const int bh = (int)(row / a.Sk), key = (int)(row - (long long)bh * a.Sk), b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    char* dst = const_cast<char*>(row_ptr(i < n ? a.dK : a.dV, b, key, hk, sizeof(T)));
+    if constexpr (sizeof(T) == 2) {
+        const u32x2_t v = {pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+        *reinterpret_cast<u32x2_t*>(dst + part * 8) = v;
+    } else {
+        *reinterpret_cast<f32x4_t*>(dst + part * 16) = acc;
+    }
+}
+
+// Tiles in order of falling cost, so that the long ones do not begin when the others are done.  One workgroup for the row tiles (cost: keys between the first and the
+// last that its rows read; forward: that its first, middle and last row read, an estimate that costs three look-ups) and, in a
+// backward call, a second one for the key tiles (cost: chunks of 32 rows that read one of its keys).  Costs are sorted into 64 classes.
+struct OrderArgs { int *order_q, *cost_q, *order_k, *cost_k; int rows_per_tile; };
+__global__ __launch_bounds__(1024) void dense_order_kernel(DenseArgs a, OrderArgs o) {
+    __shared__ int classes[64], top;
+    const bool keys = blockIdx.x == 1;
+    const int tiles = keys ? (a.Sk + DENSE_TILE_ROWS - 1) / DENSE_TILE_ROWS : (a.M + o.rows_per_tile - 1) / o.rows_per_tile, n = a.B * tiles, t = threadIdx.x;
+    const int n_chunks = (a.M + 31) / 32;
+    int *cost = keys ? o.cost_k : o.cost_q, *order = keys ? o.order_k : o.order_q;
+    if (t < 64) classes[t] = 0;
+    if (t == 0) top = 1;
+    if (keys) {                                              // +1 where a chunk's keys begin, -1 behind their end; then running sums
+        for (int i = t; i < n; i += 1024) cost[i] = 0;
+        __syncthreads();
+        for (int i = t; i < a.B * n_chunks; i += 1024) {
+            const int b = i / n_chunks;
+            const int4 r = a.row_bounds[(long long)b * a.Hkv * n_chunks + (i - b * n_chunks)];
+            if (r.x >= r.y) continue;
+            const int first = r.x / DENSE_TILE_ROWS, last = (r.y - 1) / DENSE_TILE_ROWS;
+            atomicAdd(cost + b * tiles + first, 1);
+            if (last + 1 < tiles) atomicSub(cost + b * tiles + last + 1, 1);
+        }
+        __syncthreads();
+        for (int b = t >> 6; b < a.B; b += 16) {             // a wavefront per batch element
+            int carry = 0;
+            for (int i0 = 0; i0 < tiles; i0 += 64) {
+                const int i = i0 + (t & 63);
+                int x = i < tiles ? __hip_atomic_load(cost + b * tiles + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) {
+                    const int y = __shfl_up(x, off, 64);
+                    if ((t & 63) >= off) x += y;
+                }
+                x += carry;
+                carry = __shfl(x, 63, 64);
+                if (i < tiles) cost[b * tiles + i] = x;
+            }
+        }
+    } else {
+        for (int i = t; i < n; i += 1024) {
+            const int b = i / tiles, m0 = (i - b * tiles) * o.rows_per_tile, m1 = min(m0 + o.rows_per_tile, a.M) - 1;
+            int first = INT32_MAX, end = 0;
+            if (o.cost_k) {
+                for (int c = m0 >> 5; c <= m1 >> 5; ++c) {
+                    const int4 r = a.row_bounds[(long long)b * a.Hkv * n_chunks + c];
+                    first = min(first, r.x);
+                    end = max(end, r.y);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    const int2 r = dense_range(a, b, query_of(a, k == 0 ? m0 : k == 1 ? (m0 + m1) >> 1 : m1));
+                    if (r.x < r.y) {
+                        first = min(first, r.x);
+                        end = max(end, r.y);
+                    }
+                }
+            }
+            cost[i] = max(end - first, 0) / 32;
+        }
+    }
+    __syncthreads();
+    for (int i = t; i < n; i += 1024) atomicMax(&top, cost[i]);
+    __syncthreads();
+    auto class_of = [&](int i) { return 63 - (int)((long long)min(max(cost[i], 0), top) * 63 / top); };
+    for (int i = t; i < n; i += 1024) atomicAdd(classes + class_of(i), 1);
+    __syncthreads();
+    if (t == 0) {
+        int sum = 0;
+        for (int k = 0; k < 64; ++k) {
+            const int x = classes[k];
+            classes[k] = sum;
+            sum += x;
+        }
+    }
+    __syncthreads();
+    for (int i = t; i < n; i += 1024) order[atomicAdd(classes + class_of(i), 1)] = i;
+}
+
 // What the backward kernels read of every packed row, 32 rows per workgroup, 8 lanes a row.
 template <class T, int D>
 __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     constexpr int CPL = D / 8, VEC = 16 / sizeof(T);
     __shared__ int4 bounds[32];
     const int n_chunks = (a.M + 31) / 32, bh = blockIdx.x / n_chunks, c = blockIdx.x - bh * n_chunks, b = bh / a.Hkv, hk = bh - b * a.Hkv;
-    const int r = threadIdx.x >> 3, part = threadIdx.x & 7, m = c * 32 + r, mc = min(m, a.M - 1), q = mc / a.G, h = hk * a.G + (mc - q * a.G);
+    const int r = threadIdx.x >> 3, part = threadIdx.x & 7, m = c * 32 + r, mc = min(m, a.M - 1), q = query_of(a, mc), h = hk * a.G + (mc - q * a.G);
     const char *o = row_ptr(a.O, b, q, h, sizeof(T)) + part * CPL * sizeof(T), *g = row_ptr(a.dO, b, q, h, sizeof(T)) + part * CPL * sizeof(T);
     float d = 0.f;
 #pragma unroll
@@ -98,8 +211,9 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
         float lse2 = a.LSE[((long long)b * a.Hq + h) * a.Sq + q] * DENSE_LOG2E;
         if (m >= a.M) k = make_int2(0, 0);
         if (k.x >= k.y || lse2 == -INFINITY) lse2 = INFINITY;
+        else if (!(fabsf(d) < INFINITY)) lse2 = NAN;
         info->lse2[r] = lse2;
-        info->ndelta[r] = m < a.M ? -d : 0.f;
+        info->ndelta[r] = m < a.M && fabsf(d) < INFINITY ? -d : 0.f;
         info->lo[r] = k.x;
         info->hi[r] = k.y;
         info->slope2[r] = a.slopes ? a.slopes[h] * DENSE_LOG2E : 0.f;
@@ -125,19 +239,49 @@ int splits_for(int64_t tiles, int64_t Sk) {
     return (int)std::max<int64_t>(1, std::min(by_places, by_keys));
 }
 
-struct Sizes { int G, splits; int64_t M, fwd, bwd; };
+// Row splits of the dK/dV kernel, the same with at least 256 rows each.
+int row_splits_for(int64_t tiles, int64_t M) {
+    return (int)std::max<int64_t>(1, std::min(512 / std::max<int64_t>(tiles, 1), M / 256));
+}
+// More pieces of work than run at a time: their order matters.
+bool order_matters(int64_t pieces) { return pieces > 512; }
+
+struct Sizes {
+    int G, splits, row_splits, rows_per_tile;
+    int64_t M, q_tiles, k_tiles, chunks;       // tiles and chunks of all batch elements and key heads
+    size_t part_lse, part_o, order, fwd;       // forward workspace: offsets, bytes
+    size_t info, bounds, order_b, part_b, bwd; // backward
+};
 // false: not a supported geometry
 bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, Sizes& z) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv || (D != 64 && D != 128)) return false;
     z.G = Hq / Hkv;
     if (Sq >= (1 << 24) || Sk >= (1 << 24) || Sq * z.G >= (1 << 24)) return false;
     z.M = Sq * z.G;
-    const int rows = z.M <= DENSE_FEW_ROWS ? 32 : DENSE_TILE_ROWS;
-    const int64_t tiles = (int64_t)B * Hkv * ceil_div64(z.M, rows);
-    if (tiles > (1 << 22) || (int64_t)B * Hkv * ceil_div64(Sk, 128) > (1 << 24) || (int64_t)B * Hkv * ceil_div64(z.M, 32) > (1 << 26)) return false;
-    z.splits = splits_for(tiles, Sk);
-    z.fwd = z.splits > 1 ? (int64_t)align_up((size_t)z.splits * B * Hkv * z.M * 4, 256) + (int64_t)z.splits * B * Hkv * z.M * D * 4 : 0;
-    z.bwd = (int64_t)B * Hkv * ceil_div64(z.M, 32) * (int64_t)(sizeof(RowInfo) + sizeof(int4));
+    z.rows_per_tile = z.M <= 16 ? 16 : z.M <= DENSE_FEW_ROWS ? DENSE_FEW_ROWS : DENSE_TILE_ROWS;
+    const int64_t BH = (int64_t)B * Hkv;
+    z.q_tiles = BH * ceil_div64(z.M, z.rows_per_tile);
+    z.k_tiles = BH * ceil_div64(Sk, DENSE_TILE_ROWS);
+    z.chunks = BH * ceil_div64(z.M, 32);
+    if (z.q_tiles > (1 << 22) || z.k_tiles > (1 << 22) || z.chunks > (1 << 24)) return false;
+    z.splits = splits_for(z.q_tiles, Sk);
+    z.row_splits = row_splits_for(z.k_tiles, z.M);
+    size_t off = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t at = off;
+        off += align_up((size_t)bytes, 256);
+        return at;
+    };
+    z.part_lse = take(z.splits > 1 ? z.splits * BH * z.M * 4 : 0);
+    z.part_o = take(z.splits > 1 ? z.splits * BH * z.M * D * 4 : 0);
+    z.order = take(order_matters(z.q_tiles) ? 2 * (z.q_tiles / Hkv) * 4 : 0);
+    z.fwd = std::max<size_t>(off, 256);
+    off = 0;
+    z.info = take(z.chunks * (int64_t)sizeof(RowInfo));
+    z.bounds = take(z.chunks * (int64_t)sizeof(int4));
+    z.order_b = take(2 * (B * ceil_div64(z.M, DENSE_TILE_ROWS) + z.k_tiles / Hkv) * 4);
+    z.part_b = take(z.row_splits > 1 ? 2 * z.row_splits * BH * Sk * D * 4 : 0);
+    z.bwd = off;
     return true;
 }
 
@@ -174,6 +318,7 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
     a.Sq = (int)Sq;
     a.Sk = (int)Sk;
     a.M = (int)z.M;
+    a.G_magic = z.G > 1 && z.G < 256 ? (unsigned)((((uint64_t)1 << 32) + z.G - 1) / z.G) : 0u;
     a.splits = 1;
     const float magnitude = std::fabs(how->softmax_scale);
     a.scale = how->softmax_scale;
@@ -192,8 +337,7 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
 extern "C" size_t vmoba_dense_workspace_bytes(int op, int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, int dtype) {
     Sizes z;
     if ((dtype != VMOBA_F32 && dtype != VMOBA_BF16) || !sizes_of(B, Hq, Hkv, Sq, Sk, D, z)) return 0;
-    const int64_t n = op == VMOBA_OP_ATTN_FWD ? z.fwd : op == VMOBA_OP_ATTN_BWD ? z.bwd : 0;
-    return op == VMOBA_OP_ATTN_FWD || op == VMOBA_OP_ATTN_BWD ? align_up((size_t)std::max<int64_t>(n, 256), 256) : 0;
+    return op == VMOBA_OP_ATTN_FWD ? z.fwd : op == VMOBA_OP_ATTN_BWD ? z.bwd : 0;
 }
 
 extern "C" int vmoba_key_ranges(int B, int64_t Sq, int64_t Sk, const int32_t* doc_off, int64_t doc_stride_b, int32_t n_docs, const int32_t* prefix,
@@ -215,12 +359,19 @@ extern "C" int vmoba_dense_fwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
     DenseArgs a{};
     if (const int rc = check(B, Hq, Hkv, Sq, Sk, D, Q, K, V, how, O, LSE, z, a)) return rc;
     if (!workspace || (uintptr_t)workspace & 255) return VMOBA_ERR_INVALID_ARG;
-    if (workspace_bytes < vmoba_dense_workspace_bytes(VMOBA_OP_ATTN_FWD, B, Hq, Hkv, Sq, Sk, D, Q->dtype)) return VMOBA_ERR_WORKSPACE;
+    if (workspace_bytes < z.fwd) return VMOBA_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const bool bf16 = Q->dtype == VMOBA_BF16, cap = how->cap > 0.f;
     a.splits = z.splits;
-    a.part_lse = (float*)workspace;
-    a.part_o = (float*)((char*)workspace + align_up((size_t)z.splits * B * Hkv * z.M * 4, 256));
+    char* const ws = (char*)workspace;
+    a.part_lse = (float*)(ws + z.part_lse);
+    a.part_o = (float*)(ws + z.part_o);
+    if (a.key_lo && order_matters(z.q_tiles)) {
+        int* order = (int*)(ws + z.order);
+        dense_order_kernel<<<dim3(1), dim3(1024), 0, st>>>(a, OrderArgs{order, order + z.q_tiles / Hkv, nullptr, nullptr, z.rows_per_tile});
+        VMOBA_CHECK_LAUNCH();
+        a.order_q = order;
+    }
     if (bf16) launch_dense_fwd_bf16(D, cap, st, a);
     else launch_dense_fwd_f32(D, cap, st, a);
     VMOBA_CHECK_LAUNCH();
@@ -244,24 +395,47 @@ extern "C" int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
     if (const int rc = check(B, Hq, Hkv, Sq, Sk, D, Q, K, V, how, O, LSE, z, a)) return rc;
     if (!tensor_ok(dO) || !tensor_ok(dQ) || !tensor_ok(dK) || !tensor_ok(dV) || !workspace || (uintptr_t)workspace & 255) return VMOBA_ERR_INVALID_ARG;
     if (dO->dtype != Q->dtype || dQ->dtype != Q->dtype || dK->dtype != Q->dtype || dV->dtype != Q->dtype) return VMOBA_ERR_UNSUPPORTED;
-    if (workspace_bytes < vmoba_dense_workspace_bytes(VMOBA_OP_ATTN_BWD, B, Hq, Hkv, Sq, Sk, D, Q->dtype)) return VMOBA_ERR_WORKSPACE;
+    if (workspace_bytes < z.bwd) return VMOBA_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const bool bf16 = Q->dtype == VMOBA_BF16, cap = how->cap > 0.f;
+    // packed rows of Q and dO by 32-bit offsets
+    for (const vmoba_tensor* t : {Q, dO})
+        if (!reach_ok(t, Sq) || (z.G > 1 && (t->stride_h < 0 || (uint64_t)(z.G - 1) * (uint64_t)t->stride_h * dtype_size(t->dtype) +
+                                                                      (uint64_t)Sq * (uint64_t)t->stride_s * dtype_size(t->dtype) >= ((uint64_t)1 << 32))))
+            return VMOBA_ERR_UNSUPPORTED;
     a.dO = make_view(dO);
     a.dQ = make_view(dQ);
     a.dK = make_view(dK);
     a.dV = make_view(dV);
-    const int64_t chunks = (int64_t)B * Hkv * ceil_div64(z.M, 32);
-    a.row_info = (char*)workspace;
-    a.row_bounds = (int4*)((char*)workspace + chunks * (int64_t)sizeof(RowInfo));
-    const dim3 grid((unsigned)chunks);
+    char* const ws = (char*)workspace;
+    a.row_info = ws + z.info;
+    a.row_bounds = (int4*)(ws + z.bounds);
+    a.part_o = (float*)(ws + z.part_b);
+    a.splits = z.row_splits;
+    const dim3 grid((unsigned)z.chunks);
     if (bf16 && D == 128) dense_rows_kernel<__bf16, 128><<<grid, dim3(256), 0, st>>>(a);
     else if (bf16) dense_rows_kernel<__bf16, 64><<<grid, dim3(256), 0, st>>>(a);
     else if (D == 128) dense_rows_kernel<float, 128><<<grid, dim3(256), 0, st>>>(a);
     else dense_rows_kernel<float, 64><<<grid, dim3(256), 0, st>>>(a);
     VMOBA_CHECK_LAUNCH();
+    const int64_t nq = B * ceil_div64(z.M, DENSE_TILE_ROWS), nk = z.k_tiles / Hkv;
+    if (a.key_lo && order_matters(std::max(nq, nk) * Hkv)) {
+        int* order = (int*)(ws + z.order_b);
+        dense_order_kernel<<<dim3(2), dim3(1024), 0, st>>>(a, OrderArgs{order, order + nq, order + 2 * nq, order + 2 * nq + nk, DENSE_TILE_ROWS});
+        VMOBA_CHECK_LAUNCH();
+        a.order_q = order;
+        a.order_k = order + 2 * nq;
+    }
     if (bf16) launch_dense_bwd_bf16(D, cap, st, a);
     else launch_dense_bwd_f32(D, cap, st, a);
     VMOBA_CHECK_LAUNCH();
+    if (a.splits > 1) {
+        const dim3 sums((unsigned)ceil_div64(2 * (int64_t)B * Hkv * Sk * (D / 4), 256));
+        if (bf16 && D == 128) dense_sum_kernel<__bf16, 128><<<sums, dim3(256), 0, st>>>(a);
+        else if (bf16) dense_sum_kernel<__bf16, 64><<<sums, dim3(256), 0, st>>>(a);
+        else if (D == 128) dense_sum_kernel<float, 128><<<sums, dim3(256), 0, st>>>(a);
+        else dense_sum_kernel<float, 64><<<sums, dim3(256), 0, st>>>(a);
+        VMOBA_CHECK_LAUNCH();
+    }
     return VMOBA_OK;
 }

@@ -3,27 +3,29 @@
 // them (S, dP, dV, dK: four).  Seven products for the five that a single pass with dQ in atomics would need.
 //
 // dz = P (dP - delta) (1 - tanh^2), rounded to bfloat16 for the products that follow (relative error 2^-9 a value, like P's).
-// Masked pairs: P and dz are replaced by 0, whatever the scores are; operands that the last products contract over (K rows for dQ, Q and dO rows
-// for dK and dV) lose their values that are not finite in groups with masked pairs.  A pair that does read such a value has P or delta not finite
-// and gives NaN.
+// Masked pairs: their scores are replaced (-inf, or 0 with an infinite log-sum-exp), so P and dz are 0, and tiles with masked pairs lose their values that are not finite in LDS before
+// they are multiplied -- 0 times infinity is no number.  A pair that does read such a value has a log-sum-exp or a delta that is not finite, and gives NaN.
 #include "dense_common.h"
 
 namespace {
 
-// s: x = <q, k> -> weight P; f: what P * (dP - delta) is multiplied by.
+// x = <q, k> -> weight P, from c = -(log-sum-exp + bias), base 2; f: what P (dP - delta) is multiplied by (CAP alone).
 template <bool CAP>
-__device__ __forceinline__ float weight_of(const DenseArgs& a, float x, float bias2, float lse2, float& f) {
-    float r = 0.f;
-    const float s2 = dense_score<CAP>(a, x, r);
-    f = CAP ? 4.f * r * (1.f - r) : 1.f;
-    return exp2_raw(s2 - bias2 - lse2);
+__device__ __forceinline__ float weight_of(const DenseArgs& a, float x, float c, float& f) {
+    if constexpr (CAP) {
+        const float r = __builtin_amdgcn_rcpf(1.f + exp2_raw(x * a.cap_in));
+        f = r * fmaf(-4.f, r, 4.f);
+        return exp2_raw(fmaf(-2.f * a.cap2, r, a.cap2 + c));
+    } else {
+        return exp2_raw(fmaf(x, a.scale_log2, c));
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
 // dQ: the forward kernel's decomposition; 4 wavefronts x 32 rows, chunks of 64 keys through two LDS buffers, requested one chunk ahead.
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
-    using TL = RowTile16<D>;
+    using TL = DenseTile<D>;
     constexpr int KC = 64;
     constexpr int KSTEPS = D / 32, CT = D / 16;
     constexpr int HB = TL::HB, PPR = TL::PPR, RPI = TL::RPI;
@@ -34,9 +36,10 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     __shared__ __align__(1024) char smem[2 * BUF + 64];
 
     const int tiles = (a.M + 127) / 128;
-    const int item = dense_item(a.B * a.Hkv * tiles);
-    if (item < 0) return;
-    const int tile = item % tiles, bh = item / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const DensePiece piece = dense_piece(a.B * tiles, a.Hkv);
+    if (piece.rank < 0) return;
+    const DenseTask task = dense_task(piece.rank, 1, tiles, a.order_q);
+    const int tile = task.tile, b = task.b, hk = piece.head, bh = b * a.Hkv + hk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
     const int m0 = tile * 128 + wave * 32;
@@ -49,7 +52,7 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     bf16x8_t qf[2][KSTEPS], dof[2][KSTEPS];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int m = m0 + 16 * t + l16, mc = min(m, a.M - 1), q = mc / a.G, h = hk * a.G + (mc - q * a.G);
+        const int m = m0 + 16 * t + l16, mc = min(m, a.M - 1), q = query_of(a, mc), h = hk * a.G + (mc - q * a.G);
         const RowInfo& r = info[mc >> 5];
         lo[t] = m < a.M ? r.lo[mc & 31] : 0;
         hi[t] = m < a.M ? r.hi[mc & 31] : 0;
@@ -62,7 +65,8 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
             qf[t][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(p + ks * 64) ^ a.negate);
-            dof[t][ks] = *reinterpret_cast<const bf16x8_t*>(p2 + ks * 64);
+            unsigned unused = 0;      // (what was not finite shows in the row's log-sum-exp, see dense_rows_kernel)
+            dof[t][ks] = finite_only(*reinterpret_cast<const bf16x8_t*>(p2 + ks * 64), unused);
         }
     }
     int any_lo = INT32_MAX, any_hi = 0, all_lo = 0, all_hi = INT32_MAX;
@@ -83,18 +87,20 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     }
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
     all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    int tile_lo = all_lo, tile_hi = all_hi;     // keys that all rows of the workgroup read
     {
-        int* w = reinterpret_cast<int*>(smem + 2 * BUF);
-        if (lane == 0) {
-            w[wave] = any_lo;
-            w[4 + wave] = any_hi;
-        }
+        int4* w = reinterpret_cast<int4*>(smem + 2 * BUF);
+        if (lane == 0) w[wave] = make_int4(any_lo, any_hi, all_lo, all_hi);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            any_lo = min(any_lo, w[i]);
-            any_hi = max(any_hi, w[4 + i]);
+            any_lo = min(any_lo, w[i].x);
+            any_hi = max(any_hi, w[i].y);
+            tile_lo = max(tile_lo, w[i].z);
+            tile_hi = min(tile_hi, w[i].w);
         }
+        tile_lo = __builtin_amdgcn_readfirstlane(tile_lo);
+        tile_hi = __builtin_amdgcn_readfirstlane(tile_hi);
     }
     int k_first = __builtin_amdgcn_readfirstlane(any_lo), k_end = __builtin_amdgcn_readfirstlane(any_hi);
     if (k_first >= k_end) k_first = k_end = 0;
@@ -118,68 +124,103 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     f32x4_t acc[CT][2];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) acc[ct][0] = acc[ct][1] = zero4;
-    uint32_t rlane[TL::NRB], tlane[TL::NTB];
-#pragma unroll
-    for (int i = 0; i < TL::NRB; ++i) rlane[i] = TL::row_lane(lane, i);
-#pragma unroll
-    for (int i = 0; i < TL::NTB; ++i) tlane[i] = TL::tr_lane(lane, i);
+    const uint32_t rlane = TL::row_lane(lane, 0), tlane = TL::tr_lane(lane, 0);
+    uint32_t rows0 = 0, cols0 = 0;              // lane addresses in the current chunk's buffer
 
+    // A 32-key group is a sequence of units of one LDS operand and two matrix instructions (one per 16 rows): S^T over (16 keys, k-step), dP^T over
+    // the same, the third product over the channel tiles.  Operands pass through a ring, fetched AHEAD units before use; weights are computed
+    // between the matrix instructions, those of the first 16 keys from the middle of the first phase on.  Fences keep that order.
+    constexpr int NP = 2 * KSTEPS, NSEQ = 3 * NP, AHEAD = 3, RING = AHEAD + 1;
+    static_assert(NP == CT && NSEQ % RING == 0, "as many units in each phase; the second group continues the ring where the first one left it");
+    auto fetch = [&](int mt, int n) -> bf16x8_t {      // operand of unit n of group mt (n past the end: next group)
+        if (n >= NSEQ) { mt += 1; n -= NSEQ; }
+        if (n < NP) return TL::rows(smem + mt * HB, rows0, n / KSTEPS, n % KSTEPS);
+        if (n < 2 * NP) return TL::rows(smem + (2 + mt) * HB, rows0, (n - NP) / KSTEPS, n % KSTEPS);
+        return TL::transposed(smem + mt * HB, cols0, n - 2 * NP);
+    };
     if (n_chunks > 0) request(0);
     VMOBA_WAIT_VMCNT(0);
     __syncthreads();
-    unsigned found = 0;
     for (int c = 0; c < n_chunks; ++c) {
         const uint32_t buf = (uint32_t)(c & 1) * BUF;
+        const int kc = k_first + c * KC;
+        if (__builtin_expect(kc < tile_lo || kc + KC > tile_hi, 0)) {
+            clean_tile(smem + buf, BUF, 256);
+            __syncthreads();
+        }
         if (c + 1 < n_chunks) request(c + 1);
+        rows0 = rlane + buf;
+        cols0 = tlane + buf;
+        bf16x8_t op[RING];
+#pragma unroll
+        for (int n = 0; n < RING; ++n) op[n] = fetch(0, n < AHEAD ? n : 0);
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
-            const int kb = k_first + c * KC + mt * 32;
-            if (kb >= k_end) break;
-            const bool masked = kb < all_lo || kb + 32 > all_hi;
-            f32x4_t s[2][2], dp[2][2];            // [16 keys][16 rows]: value i is key 16 * kt + 4 * g + i
+            const int kb = kc + mt * 32;
+            if (kb < k_end) {
+                const bool masked = kb < all_lo || kb + 32 > all_hi;
+                f32x4_t s[2][2], dp[2][2];            // [16 keys][16 rows]: value i is key 16 * kt + 4 * g + i
+                bf16x8_t ds[2];
+                float rel[2];
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+                for (int t = 0; t < 2; ++t) rel[t] = BIAS ? (float)(row_pos[t] - kb - 4 * g) : 0.f;
+                auto p_value = [&](int v) {           // S^T -> P^T (1 - tanh^2), in place
+                    const int kt = v >> 3, t = (v >> 2) & 1, i = v & 3;
+                    float f = 1.f, c2 = -lse2[t];
+                    if constexpr (BIAS) c2 = fmaf(-slope2[t], fabsf(rel[t] - (float)(16 * kt + i)), c2);
+                    float p = weight_of<CAP>(a, s[kt][t][i], c2, f);
+                    if constexpr (CAP) p *= f;
+                    s[kt][t][i] = p;
+                };
+                auto ds_value = [&](int v) {
+                    const int kt = v >> 3, t = (v >> 2) & 1, i = v & 3;
+                    float d = s[kt][t][i] * dp[kt][t][i];
+                    asm volatile("" : "+v"(d));
+                    s[kt][t][i] = d;
+                };
 #pragma unroll
-                for (int ks = 0; ks < KSTEPS; ++ks) {
-                    const bf16x8_t x = TL::rows(smem, rlane, buf + mt * HB, kt, ks);
+                for (int n = 0; n < NSEQ; ++n) {
+                    // (the group after the second one waits for the next chunk)
+                    if (n + AHEAD < NSEQ || mt == 0) op[(n + AHEAD) % RING] = fetch(mt, n + AHEAD);
+                    const int m = n % NP, kt = m / KSTEPS, ks = m % KSTEPS;
+                    if ((n == KSTEPS + 1 || n == NP) && __builtin_expect(masked, 0)) {      // the scores of the first, of the second 16 keys are complete
+                        const int half = n == NP ? 1 : 0;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) s[kt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, qf[t][ks], ks == 0 ? zero4 : s[kt][t], 0, 0, 0);
-                }
+                        for (int t = 0; t < 2; ++t) {
+                            const int first_key = lo[t] - kb - 4 * g - 16 * half, end = hi[t] - kb - 4 * g - 16 * half;
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int ks = 0; ks < KSTEPS; ++ks) {
-                    const bf16x8_t x = TL::rows(smem, rlane, buf + (2 + mt) * HB, kt, ks);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) dp[kt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, dof[t][ks], ks == 0 ? ndl[t] : dp[kt][t], 0, 0, 0);
-                }
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const float rel = BIAS ? (float)(row_pos[t] - kb - 4 * g) : 0.f;
-                const int first_key = lo[t] - kb - 4 * g, end = hi[t] - kb - 4 * g;
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float f;
-                        const float p = weight_of<CAP>(a, s[kt][t][i], BIAS ? slope2[t] * fabsf(rel - (float)(16 * kt + i)) : 0.f, lse2[t], f);
-                        float d = p * f * dp[kt][t][i];
-                        if (masked && (16 * kt + i < first_key || 16 * kt + i >= end)) d = 0.f;
-                        s[kt][t][i] = d;
+                            for (int i = 0; i < 4; ++i)
+                                if (i < first_key || i >= end) s[half][t][i] = -INFINITY;      // (with the cap: r = 1, so f = 0)
+                        }
                     }
-            }
-            bf16x8_t ds[2];
+                    if (n == 2 * NP) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const float d8[8] = {s[0][t][0], s[0][t][1], s[0][t][2], s[0][t][3], s[1][t][0], s[1][t][1], s[1][t][2], s[1][t][3]};
-                ds[t] = pack8(d8);
-            }
+                        for (int v = 8; v < 16; ++v) ds_value(v);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                bf16x8_t x = TL::transposed(smem, tlane, buf + mt * HB, ct);
-                if (masked) x = finite_only(x, found);
+                        for (int t = 0; t < 2; ++t) {
+                            const float d8[8] = {s[0][t][0], s[0][t][1], s[0][t][2], s[0][t][3], s[1][t][0], s[1][t][1], s[1][t][2], s[1][t][3]};
+                            ds[t] = pack8(d8);
+                        }
+                    }
 #pragma unroll
-                for (int t = 0; t < 2; ++t) acc[ct][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, ds[t], acc[ct][t], 0, 0, 0);
+                    for (int t = 0; t < 2; ++t) {
+                        if (n < NP)
+                            s[kt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[n % RING], qf[t][ks], ks == 0 ? zero4 : s[kt][t], 0, 0, 0);
+                        else if (n < 2 * NP)
+                            dp[kt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[n % RING], dof[t][ks], ks == 0 ? ndl[t] : dp[kt][t], 0, 0, 0);
+                        else
+                            acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[n % RING], ds[t], acc[m][t], 0, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    constexpr int E0 = KSTEPS + 1, E1 = NP;             // units of the first 8 weights
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) {
+                        if (E0 + v * (E1 - E0) / 8 == n) p_value(v);
+                        if (NP + v * NP / 8 == n) p_value(8 + v);
+                        if (NP + KSTEPS + v * KSTEPS / 8 == n) ds_value(v);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
         VMOBA_WAIT_VMCNT(0);
@@ -201,7 +242,7 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     for (int k = 0; k < 32 * PPR / 64; ++k) {
         const int row = k * (64 / PPR) + lane / PPR, m = m0 + row;
         if (m < a.M) {
-            const int q = m / a.G, h = hk * a.G + (m - q * a.G);
+            const int q = query_of(a, m), h = hk * a.G + (m - q * a.G);
             *reinterpret_cast<u32x4_t*>(const_cast<char*>(row_ptr(a.dQ, b, q, h, 2)) + lane % PPR * 16) =
                 *reinterpret_cast<const u32x4_t*>(mine + row * OPITCH + lane % PPR * 16);
         }
@@ -218,7 +259,7 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
 // Which chunks those are stands in row_bounds: a wavefront looks at 64 of them at a time.
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
-    using TL = RowTile16<D>;
+    using TL = DenseTile<D>;
     constexpr int KSTEPS = D / 32, CT = D / 16;
     constexpr int HB = TL::HB, PPR = TL::PPR, RPI = TL::RPI;
     constexpr int BUF = 2 * HB + (int)sizeof(RowInfo);   // 32 rows of Q, of dO, and what is known of them
@@ -229,16 +270,17 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
     __shared__ __align__(1024) char smem[B0 + 2 * BUF];
 
     const int tiles = (a.Sk + 127) / 128;
-    const int item = dense_item(a.B * a.Hkv * tiles);
-    if (item < 0) return;
-    const int tile = item % tiles, bh = item / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
+    if (piece.rank < 0) return;
+    const DenseTask task = dense_task(piece.rank, a.splits, tiles, a.order_k);
+    const int tile = task.tile, b = task.b, hk = piece.head, bh = b * a.Hkv + hk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
     const int k0 = tile * 128, kw = k0 + wave * 32;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     const int n_chunks = (a.M + 31) / 32;
     const char* info = a.row_info + (long long)bh * n_chunks * (long long)sizeof(RowInfo);
-    const int4* bounds = a.row_bounds + (long long)bh * n_chunks;
+    ChunkWalk walk(a.row_bounds + (long long)bh * n_chunks, n_chunks, k0, k0 + 128, lane, task.split, a.splits);
 
     // K fragments of the wavefront's keys (column l16 of 16-key half kt), V rows of the workgroup's
     bf16x8_t kf[2][KSTEPS];
@@ -248,149 +290,176 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) kf[kt][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(p + ks * 64) ^ a.negate);
     }
-    uint32_t pc16[TL::NPC];
-#pragma unroll
-    for (int i = 0; i < TL::NPC; ++i) pc16[i] = TL::request_piece(lane, i);
     const char* vbase = row_ptr(a.V, b, 0, hk, 2);
 #pragma unroll
     for (int i = 0; i < 4 * IPW; ++i)
-        dma_row16<0>(vbase, (uint32_t)min(kw + i * RPI + lane / PPR, a.Sk - 1), (uint32_t)(a.V.stride_s * 2), pc16[i % TL::NPC], lds0 + (uint32_t)(wave * 4 * IPW + i) * 1024);
+        dma_row16<0>(vbase, (uint32_t)min(kw + i * RPI + lane / PPR, a.Sk - 1), (uint32_t)(a.V.stride_s * 2), TL::request_piece(lane, i % TL::NPC), lds0 + (uint32_t)(wave * 4 * IPW + i) * 1024);
 
+    const char *qbase = row_ptr(a.Q, b, 0, hk * a.G, 2), *obase = row_ptr(a.dO, b, 0, hk * a.G, 2);
+    const uint32_t qss = (uint32_t)(a.Q.stride_s * 2), qsh = (uint32_t)(a.Q.stride_h * 2), oss = (uint32_t)(a.dO.stride_s * 2), osh = (uint32_t)(a.dO.stride_h * 2);
     auto request = [&](int c, int par) {
         const uint32_t l = lds0 + B0 + (uint32_t)par * BUF;
 #pragma unroll
         for (int i = 0; i < IPW; ++i) {
-            const int m = min(c * 32 + (wave * IPW + i) * RPI + lane / PPR, a.M - 1), q = m / a.G, h = hk * a.G + (m - q * a.G);
-            dma16_at(row_ptr(a.Q, b, q, h, 2) + pc16[i % TL::NPC], l + (uint32_t)(wave * IPW + i) * 1024);
-            dma16_at(row_ptr(a.dO, b, q, h, 2) + pc16[i % TL::NPC], l + HB + (uint32_t)(wave * IPW + i) * 1024);
+            const int m = min(c * 32 + (wave * IPW + i) * RPI + lane / PPR, a.M - 1);
+            const uint32_t piece = TL::request_piece(lane, i);
+            dma16(qbase, packed_row(a, m, qss, qsh) + piece, l + (uint32_t)(wave * IPW + i) * 1024);
+            dma16(obase, packed_row(a, m, oss, osh) + piece, l + HB + (uint32_t)(wave * IPW + i) * 1024);
         }
-        if (wave == 3) dma16_at(info + (long long)c * (long long)sizeof(RowInfo) + lane * 16, l + 2 * HB);
+        if (wave == 3) dma16(info + (long long)c * (long long)sizeof(RowInfo), (uint32_t)lane * 16, l + 2 * HB);
     };
-    // chunks whose rows read one of the 128 keys, in order; the same for all wavefronts
-    int window = 0;
-    unsigned long long pending = 0;
-    auto look = [&]() {
-        const int c = window + lane;
-        const int4 r = c < n_chunks ? bounds[c] : make_int4(INT32_MAX, 0, 0, 0);
-        pending = __builtin_amdgcn_ballot_w64(r.x < k0 + 128 && r.y > k0);
-    };
-    auto next_chunk = [&]() {
-        while (pending == 0) {
-            window += 64;
-            if (window >= n_chunks) return -1;
-            look();
-        }
-        const int i = __builtin_ctzll(pending);
-        pending &= pending - 1;
-        return window + i;
-    };
-    look();
 
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
     f32x4_t dv[CT][2], dk[CT][2];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) dv[ct][0] = dv[ct][1] = dk[ct][0] = dk[ct][1] = zero4;
-    uint32_t rlane[TL::NRB], tlane[TL::NTB];
-#pragma unroll
-    for (int i = 0; i < TL::NRB; ++i) rlane[i] = TL::row_lane(lane, i);
-#pragma unroll
-    for (int i = 0; i < TL::NTB; ++i) tlane[i] = TL::tr_lane(lane, i);
-    const uint32_t vrows = (uint32_t)wave * HB;
+    const uint32_t rlane = TL::row_lane(lane, 0), tlane = TL::tr_lane(lane, 0);
 
-    int c = next_chunk(), par = 0;
+    // A chunk is a sequence of units: S over (16 rows, k-step), one operand and two matrix instructions (one per 16 keys) each; dP over the k-steps, four operands (V of both key
+    // halves, dO of both row halves) and four; dV over the channel tiles, dK over the channel tiles, one and two.  Weights are computed in the second half of the
+    // first phase and in the second one, dz in the third.
+    constexpr int NP = 2 * KSTEPS;
+    static_assert(NP == CT, "as many units in the first phase as in the last two");
+    int c = walk.next(), par = 0;
     if (c >= 0) request(c, 0);
     VMOBA_WAIT_VMCNT(0);
     __syncthreads();
-    unsigned found = 0;
+    clean_tile(smem, 4 * HB, 256);             // V: a value that is not finite shows in the log-sum-exp or delta of the rows that read it
+    __syncthreads();
     while (c >= 0) {
-        const int c_next = next_chunk();
-        if (c_next >= 0) request(c_next, par ^ 1);
+        const int all_lo = walk.all_lo, all_hi = walk.all_hi;
         const uint32_t buf = B0 + (uint32_t)par * BUF;
         const RowInfo* ri = reinterpret_cast<const RowInfo*>(smem + buf + 2 * HB);
-        const int4 bd = bounds[c];
-        const int all_lo = __builtin_amdgcn_readfirstlane(bd.z), all_hi = __builtin_amdgcn_readfirstlane(bd.w);
         const bool masked = kw < all_lo || kw + 32 > all_hi;
-        f32x4_t s[2][2], dp[2][2];                        // [16 rows][16 keys]: value i is row 16 * t + 4 * g + i
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int ks = 0; ks < KSTEPS; ++ks) {
-                const bf16x8_t x = TL::rows(smem, rlane, buf, t, ks);
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt) s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, kf[kt][ks], ks == 0 ? zero4 : s[t][kt], 0, 0, 0);
-            }
-        f32x4_t nd[2], lse2[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            nd[t] = *reinterpret_cast<const f32x4_t*>(ri->ndelta + 16 * t + 4 * g);
-            lse2[t] = *reinterpret_cast<const f32x4_t*>(ri->lse2 + 16 * t + 4 * g);
+        if (__builtin_expect(k0 < all_lo || k0 + 128 > all_hi, 0)) {
+            clean_tile(smem + buf, 2 * HB, 256);
+            __syncthreads();
         }
+        const int c_next = walk.next();
+        if (c_next >= 0) request(c_next, par ^ 1);
+        const uint32_t rows0 = rlane + buf, cols0 = tlane + buf, vrows0 = pinned(rlane) + (uint32_t)wave * HB;
+        f32x4_t s[2][2], dp[2][2];                        // [16 rows][16 keys]: value i is row 16 * t + 4 * g + i
+        unsigned pw[2][4];                                // P as packed pairs
+        auto p_pair = [&](int j) {                        // values 2 j and 2 j + 1: S -> P (packed), P (1 - tanh^2) in its place
+            const int t = j >> 2, kt = (j >> 1) & 1, i0 = (j & 1) * 2, r0 = 16 * t + 4 * g + i0, key = kw + 16 * kt + l16;
+            f32x2_t l2 = *reinterpret_cast<const f32x2_t*>(ri->lse2 + r0);
+            float p[2];
+            if (__builtin_expect(masked, 0)) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (key < ri->lo[r0 + e] || key >= ri->hi[r0 + e]) {
+                        s[t][kt][i0 + e] = 0.f;
+                        l2[e] = INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float f = 1.f, c2 = -l2[e];
+                if constexpr (BIAS) c2 = fmaf(-ri->slope2[r0 + e], fabsf((float)(ri->pos[r0 + e] - key)), c2);
+                p[e] = weight_of<CAP>(a, s[t][kt][i0 + e], c2, f);
+                s[t][kt][i0 + e] = CAP ? p[e] * f : p[e];
+            }
+            pw[kt][2 * t + (j & 1)] = pack_bf16x2(p[0], p[1]);
+        };
+        auto ds_value = [&](int v) {
+            const int t = v >> 3, kt = (v >> 2) & 1, i = v & 3;
+            dp[t][kt][i] *= s[t][kt][i];
+        };
+        bf16x8_t op[4];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) op[n] = TL::rows(smem, rows0, n / KSTEPS, n % KSTEPS);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+            const int t = n / KSTEPS, ks = n % KSTEPS;
+            if (n + 3 < NP) op[(n + 3) & 3] = TL::rows(smem, rows0, (n + 3) / KSTEPS, (n + 3) % KSTEPS);
+            else if (n + 3 < NP + 2) op[(n + 3) & 3] = TL::rows(smem, vrows0, n + 3 - NP, 0);
+            else op[(n + 3) & 3] = TL::rows(smem + HB, rows0, 0, 0);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[n & 3], kf[kt][ks], ks == 0 ? zero4 : s[t][kt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int E0 = KSTEPS + 1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (E0 + j * (NP - E0) / 4 == n) p_pair(j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // V of the first and of the second 16 keys, dO of the first 16 rows; dO of the others is fetched in the unit
+        bf16x8_t v0 = op[NP & 3], v1 = op[(NP + 1) & 3], x0 = op[(NP + 2) & 3];
+        f32x4_t nd[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) nd[t] = *reinterpret_cast<const f32x4_t*>(ri->ndelta + 16 * t + 4 * g);
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
-            const bf16x8_t v0 = TL::rows(smem, rlane, vrows, 0, ks), v1 = TL::rows(smem, rlane, vrows, 1, ks);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const bf16x8_t x = TL::rows(smem, rlane, buf + HB, t, ks);
-                dp[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, v0, ks == 0 ? nd[t] : dp[t][0], 0, 0, 0);
-                dp[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, v1, ks == 0 ? nd[t] : dp[t][1], 0, 0, 0);
+            const bf16x8_t x1 = TL::rows(smem + HB, rows0, 1, ks);
+            dp[0][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x0, v0, ks == 0 ? nd[0] : dp[0][0], 0, 0, 0);
+            dp[0][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x0, v1, ks == 0 ? nd[0] : dp[0][1], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (ks + 1 < KSTEPS) x0 = TL::rows(smem + HB, rows0, 0, ks + 1);
+            else x0 = TL::transposed(smem + HB, cols0, 0);
+            if (KSTEPS == 4 || ks == 0) p_pair(KSTEPS == 4 ? 4 + ks : 4);
+            if (KSTEPS == 2 && ks == 1) p_pair(6);
+            __builtin_amdgcn_sched_barrier(0);
+            dp[1][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x1, v0, ks == 0 ? nd[1] : dp[1][0], 0, 0, 0);
+            dp[1][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x1, v1, ks == 0 ? nd[1] : dp[1][1], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (ks + 1 < KSTEPS) {
+                v0 = TL::rows(smem, vrows0, 0, ks + 1);
+                v1 = TL::rows(smem, vrows0, 1, ks + 1);
+            } else {
+                v0 = TL::transposed(smem + HB, cols0, 1);
             }
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x4_t slope2 = zero4;
-            u32x4_t pos = {0u, 0u, 0u, 0u}, lo = pos, hi = pos;
-            if constexpr (BIAS) {
-                slope2 = *reinterpret_cast<const f32x4_t*>(ri->slope2 + 16 * t + 4 * g);
-                pos = *reinterpret_cast<const u32x4_t*>(ri->pos + 16 * t + 4 * g);
-            }
-            if (masked) {
-                lo = *reinterpret_cast<const u32x4_t*>(ri->lo + 16 * t + 4 * g);
-                hi = *reinterpret_cast<const u32x4_t*>(ri->hi + 16 * t + 4 * g);
-            }
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                const int key = kw + 16 * kt + l16;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float f;
-                    float p = weight_of<CAP>(a, s[t][kt][i], BIAS ? slope2[i] * fabsf((float)((int)pos[i] - key)) : 0.f, lse2[t][i], f);
-                    float d = p * f * dp[t][kt][i];
-                    if (masked) {
-                        const bool reads = key >= (int)lo[i] && key < (int)hi[i];
-                        // (a row of dO that is not finite shows in delta; its values are taken out of the product below)
-                        p = !reads ? 0.f : fabsf(nd[t][i]) < INFINITY ? p : NAN;
-                        d = reads ? d : 0.f;
-                    }
-                    s[t][kt][i] = p;
-                    dp[t][kt][i] = d;
-                }
-            }
+            if (KSTEPS == 2) p_pair(ks == 0 ? 5 : 7);
+            __builtin_amdgcn_sched_barrier(0);
         }
         bf16x8_t pf[2], df[2];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const float p8[8] = {s[0][kt][0], s[0][kt][1], s[0][kt][2], s[0][kt][3], s[1][kt][0], s[1][kt][1], s[1][kt][2], s[1][kt][3]};
-            const float d8[8] = {dp[0][kt][0], dp[0][kt][1], dp[0][kt][2], dp[0][kt][3], dp[1][kt][0], dp[1][kt][1], dp[1][kt][2], dp[1][kt][3]};
-            pf[kt] = pack8(p8);
-            df[kt] = pack8(d8);
-        }
+        for (int kt = 0; kt < 2; ++kt) pf[kt] = __builtin_bit_cast(bf16x8_t, u32x4_t{pw[kt][0], pw[kt][1], pw[kt][2], pw[kt][3]});
+        op[0] = x0;
+        op[1] = v0;
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            bf16x8_t x = TL::transposed(smem, tlane, buf + HB, ct), y = TL::transposed(smem, tlane, buf, ct);
-            if (masked) {
-                x = finite_only(x, found);
-                y = finite_only(y, found);
+        for (int n = 0; n < 2 * CT; ++n) {
+            const int ct = n % CT, n2 = n + 2;
+            if (n2 < 2 * CT) op[n2 & 3] = TL::transposed(n2 < CT ? smem + HB : smem, cols0, n2 % CT);
+            if (n == CT) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    const float d8[8] = {dp[0][kt][0], dp[0][kt][1], dp[0][kt][2], dp[0][kt][3], dp[1][kt][0], dp[1][kt][1], dp[1][kt][2], dp[1][kt][3]};
+                    df[kt] = pack8(d8);
+                }
             }
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
-                dv[ct][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pf[kt], dv[ct][kt], 0, 0, 0);
-                dk[ct][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, df[kt], dk[ct][kt], 0, 0, 0);
+                if (n < CT) dv[ct][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[n & 3], pf[kt], dv[ct][kt], 0, 0, 0);
+                else dk[ct][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[n & 3], df[kt], dk[ct][kt], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (n < CT) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (v * CT / 16 == n) ds_value(v);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         VMOBA_WAIT_VMCNT(0);
         __syncthreads();
         c = c_next;
         par ^= 1;
+    }
+    if (a.splits > 1) {                                   // this split's sums, added up by dense_sum_kernel
+        const long long n = (long long)a.B * a.Hkv * a.Sk;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const int key = kw + 16 * kt + l16;
+            if (key < a.Sk) {
+                float* dst = a.part_o + (2 * task.split * n + (long long)bh * a.Sk + key) * D + 4 * g;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    *reinterpret_cast<f32x4_t*>(dst + 16 * ct) = dk[ct][kt] * a.scale;
+                    *reinterpret_cast<f32x4_t*>(dst + n * D + 16 * ct) = dv[ct][kt];
+                }
+            }
+        }
+        return;
     }
     char* mine = smem + wave * 32 * OPITCH;
 #pragma unroll
@@ -423,7 +492,7 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
 
 template <int D>
 void launch_bwd(bool cap, hipStream_t st, const DenseArgs& a) {
-    const dim3 gq(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.M, 128))), gk(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.Sk, 128))), block(256);
+    const dim3 gq(dense_grid((int64_t)a.B * ceil_div64(a.M, 128), a.Hkv)), gk(dense_grid((int64_t)a.B * ceil_div64(a.Sk, 128) * a.splits, a.Hkv)), block(256);
 #define BOTH(CAP, BIAS)                                     \
     do {                                                    \
         dense_dq_kernel<D, CAP, BIAS><<<gq, block, 0, st>>>(a);   \

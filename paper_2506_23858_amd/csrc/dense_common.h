@@ -20,25 +20,57 @@ struct DenseArgs {
     long long q_first;
     float* LSE;
     float *part_o, *part_lse;      // forward, more than one split: [splits][B * Hkv][M][D] and [splits][B * Hkv][M] (base 2)
+    const int *order_q, *order_k;  // places by falling cost: [B * row tiles] and, backward, [B * key tiles]; null: as they come
     char* row_info;                // backward: ROW_INFO bytes per 32 rows, see RowInfo
     int4* row_bounds;              // backward: {lowest lo, highest hi, highest lo, lowest hi} of every 32 rows with keys
     int B, Hq, Hkv, G, Sq, Sk, M;
-    int splits;
+    int splits;                    // of a tile's keys (forward), of a key tile's rows (dK/dV)
     float scale, scale_log2;       // softmax_scale; max(|softmax_scale| log2 e, FLT_MIN)
     float cap2, cap_in, cap_arg;   // cap log2(e); 2 scale_log2 / cap; |softmax_scale| / cap
+    unsigned G_magic;              // see query_of; 0: divide
     unsigned negate;               // 0x80008000 for a negative scale (bfloat16 pairs)
 };
 
 // What the dK/dV kernel needs to know of 32 consecutive rows, one 1 KB request: arrays of 32 words.
 struct RowInfo {
-    float lse2[32];        // log-sum-exp of the row, base 2; +inf for a row without keys (all its weights are then 0)
-    float ndelta[32];      // -rowsum(dO * O)
+    float lse2[32];        // log-sum-exp of the row, base 2; +inf for a row without keys (all its weights are then 0), NaN for a row whose delta is
+                           // not finite (its weights are then NaN)
+    float ndelta[32];      // -rowsum(dO * O), finite
     int lo[32], hi[32];    // its keys
     float slope2[32];      // slope * log2(e)
     int pos[32];           // its position
     int pad[64];
 };
 static_assert(sizeof(RowInfo) == 1024, "one request of 64 lanes x 16 bytes");
+
+// Operands of a RowTile16 from one address per lane and tile: k-step ks and channel tile ct only turn bits of the piece position, and a tile lies at a multiple
+// of 256 bytes, so they are an exclusive-or with lane address + tile place (twelve addresses of their own would take twelve registers).
+template <int D>
+struct DenseTile : RowTile16<D> {
+    using Base = RowTile16<D>;
+    __device__ static __forceinline__ bf16x8_t rows(const char* base, uint32_t at, int kt, int ks) {
+        return *reinterpret_cast<const bf16x8_t*>(base + (at ^ (uint32_t)(ks * 64)) + kt * 16 * Base::RB);
+    }
+    __device__ static __forceinline__ bf16x8_t transposed(const char* base, uint32_t at, int ct) {
+        const char* p = base + (at ^ (uint32_t)(ct * 32));
+        const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + 16 * Base::RB));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+// A value the compiler may not take out of the loop (it would keep all addresses that follow from it in registers).
+__device__ __forceinline__ uint32_t pinned(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+// m / G for a packed row m < 2^24 (magic = ceil(2^32 / G) for 1 < G < 256: the error of the product stays below 1 / G)
+__device__ __forceinline__ int query_of(const DenseArgs& a, int m) {
+    return a.G == 1 ? m : a.G_magic ? (int)__umulhi((unsigned)m, a.G_magic) : m / a.G;
+}
+
+// Byte offset of packed row m of Q or dO from its first one (the host has checked that 32 bits reach): q * ss + g * sh = m * sh + q * (ss - G * sh).
+__device__ __forceinline__ uint32_t packed_row(const DenseArgs& a, int m, uint32_t ss, uint32_t sh) {
+    return a.G == 1 ? (uint32_t)m * ss : (uint32_t)m * sh + (uint32_t)query_of(a, m) * (ss - (uint32_t)a.G * sh);
+}
 
 // Key range of row m's query, within 0 .. Sk; {0, 0} if it has none.
 __device__ __forceinline__ int2 dense_range(const DenseArgs& a, int b, int q) {
@@ -99,7 +131,7 @@ __device__ __forceinline__ void dense_repair(const DenseArgs& a, int b, int hk, 
                 const int rl = __shfl(r < 16 ? lo_a : lo_b, r & 15, 64), rh = __shfl(r < 16 ? hi_a : hi_b, r & 15, 64);
                 const float lse2 = __shfl(r < 16 ? lse_a : lse_b, r & 15, 64);
                 if (m >= a.M || key < rl || key >= rh) continue;
-                const int q = m / a.G, h = hk * a.G + (m - q * a.G);
+                const int q = query_of(a, m), h = hk * a.G + (m - q * a.G);
                 const T* qrow = (const T*)row_ptr(a.Q, b, q, h, ES) + lane * CPL;
                 float x = 0.f;
 #pragma unroll
@@ -125,13 +157,66 @@ __device__ __forceinline__ void dense_repair(const DenseArgs& a, int b, int hk, 
         }
     }
 }
-// Workgroup ids go round the 8 XCDs: XCD x = id % 8 takes the x-th eighth of `total` items, so that the tiles of one key head share
-// an L2.  -1: this workgroup has none.
-__device__ __forceinline__ int dense_item(int total) {
-    const int per = (total + 7) >> 3, slot = (int)(blockIdx.x >> 3), f = (int)(blockIdx.x & 7) * per + slot;
-    return slot < per && f < total ? f : -1;
+// The chunks of 32 packed rows that read any key of first .. end - 1, in order (the same for all wavefronts of a workgroup).  A wavefront looks at the bounds of 64 of
+// them at a time and keeps those of the chunk it returned, so that the walk's loop holds no load of its own.  Split s of several takes every splits-th chunk.
+struct ChunkWalk {
+    const int4* bounds;
+    int n, first, end, lane, split, splits, window = -64;
+    unsigned long long pending = 0;
+    int4 mine;
+    int all_lo, all_hi;      // of the chunk that next() returned: keys that all its rows read
+    __device__ __forceinline__ ChunkWalk(const int4* b, int chunks, int k0, int k1, int l, int s, int ss)
+        : bounds(b), n(chunks), first(k0), end(k1), lane(l), split(s), splits(ss) {}
+    __device__ __forceinline__ int next() {
+        while (pending == 0) {
+            window += 64;
+            if (window >= n) return -1;
+            const int c = window + lane;
+            mine = c < n ? bounds[c] : make_int4(INT32_MAX, 0, 0, 0);
+            pending = __builtin_amdgcn_ballot_w64(mine.x < end && mine.y > first && (splits == 1 || c % splits == split));
+        }
+        const int i = __builtin_ctzll(pending);
+        pending &= pending - 1;
+        all_lo = __builtin_amdgcn_readlane(mine.z, i);
+        all_hi = __builtin_amdgcn_readlane(mine.w, i);
+        return window + i;
+    }
+};
+// A tile in LDS loses its values that are not finite (bfloat16, `bytes` of it, by `threads` threads); whether this thread met any.
+__device__ __forceinline__ bool clean_tile(char* tile, int bytes, int threads) {
+    unsigned found = 0;
+    for (int i = (int)threadIdx.x * 16; i < bytes; i += threads * 16) {
+        bf16x8_t* p = reinterpret_cast<bf16x8_t*>(tile + i);
+        *p = finite_only(*p, found);
+    }
+    return found != 0;
 }
-static inline unsigned dense_grid(int64_t total) { return (unsigned)(ceil_div64(total, 8) * 8); }
+// Which work a workgroup does.  There are `ranks` pieces for each of `heads` key heads, the costliest first where it matters (see dense_order_kernel).  Workgroup
+// ids go round the 8 XCDs and each XCD has an L2 of its own, so XCD x = id % 8 takes heads / 8 heads as a whole, rank by rank; of the rem = heads % 8 heads left
+// over, rank r's go to XCDs (r rem + 0 .. rem - 1) % 8, which gives every XCD the same number in P = 8 / gcd(rem, 8) ranks.
+__host__ __device__ constexpr int dense_period(int rem) { return rem == 0 ? 1 : rem & 1 ? 8 : rem & 2 ? 4 : 2; }
+static inline unsigned dense_grid(int64_t ranks, int heads) {
+    const int P = dense_period(heads & 7);
+    return (unsigned)(8 * ceil_div64(ranks, P) * ((heads >> 3) * P + (heads & 7) * P / 8));
+}
+struct DensePiece { int rank, head; };      // rank -1: none
+__device__ __forceinline__ DensePiece dense_piece(int ranks, int heads) {
+    const int x = (int)(blockIdx.x & 7), s = (int)(blockIdx.x >> 3), full = heads >> 3, rem = heads & 7, P = dense_period(rem), C = full * P + rem * P / 8;
+    int r = s / C * P, w = s % C;
+    for (;; ++r) {
+        const int j = (x - r * rem) & 7;             // the head left over that this XCD would take of rank r
+        const int n = full + (j < rem ? 1 : 0);
+        if (w < n) return r < ranks ? DensePiece{r, w < full ? x * full + w : 8 * full + j} : DensePiece{-1, 0};
+        w -= n;
+    }
+}
+
+// The (batch element, tile) of a rank, and its split.
+struct DenseTask { int b, tile, split; };
+__device__ __forceinline__ DenseTask dense_task(int rank, int splits, int tiles, const int* order) {
+    const int place = rank / splits, bt = order ? order[place] : place, b = bt / tiles;
+    return {b, bt - b * tiles, rank - place * splits};
+}
 
 // Most rows of a tile that one wavefront takes alone, and the rows of the tile of four.
 constexpr int DENSE_FEW_ROWS = 32, DENSE_TILE_ROWS = 128;

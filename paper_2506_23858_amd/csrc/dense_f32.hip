@@ -137,11 +137,12 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
     __shared__ __align__(16) float smem[2 * TILE];
     __shared__ int words[2 * NW];
     const int tiles = (a.M + 32 * NW - 1) / (32 * NW);
-    const int item = dense_item(a.B * a.Hkv * tiles * a.splits);
-    if (item < 0) return;
-    const int split = item % a.splits, tile = item / a.splits % tiles, bh = item / a.splits / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
+    if (piece.rank < 0) return;
+    const DenseTask task = dense_task(piece.rank, a.splits, tiles, a.order_q);
+    const int split = task.split, tile = task.tile, b = task.b, hk = piece.head, bh = b * a.Hkv + hk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
-    const int m0 = tile * 32 * NW + wave * 32, m = m0 + l32, mc = min(m, a.M - 1), q = mc / a.G, h = hk * a.G + (mc - q * a.G);
+    const int m0 = tile * 32 * NW + wave * 32, m = m0 + l32, mc = min(m, a.M - 1), q = query_of(a, mc), h = hk * a.G + (mc - q * a.G);
     const float scl = a.negate ? -a.scale_log2 : a.scale_log2;
     const int2 range = dense_range(a, b, q);
     const int lo = m < a.M ? range.x : 0, hi = m < a.M ? range.y : 0;
@@ -241,11 +242,12 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     __shared__ __align__(16) float smem[2 * TILE];
     __shared__ int words[8];
     const int tiles = (a.M + 127) / 128;
-    const int item = dense_item(a.B * a.Hkv * tiles);
-    if (item < 0) return;
-    const int tile = item % tiles, bh = item / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const DensePiece piece = dense_piece(a.B * tiles, a.Hkv);
+    if (piece.rank < 0) return;
+    const DenseTask task = dense_task(piece.rank, 1, tiles, a.order_q);
+    const int tile = task.tile, b = task.b, hk = piece.head, bh = b * a.Hkv + hk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
-    const int m = tile * 128 + wave * 32 + l32, mc = min(m, a.M - 1), q = mc / a.G, h = hk * a.G + (mc - q * a.G);
+    const int m = tile * 128 + wave * 32 + l32, mc = min(m, a.M - 1), q = query_of(a, mc), h = hk * a.G + (mc - q * a.G);
     const float scl = a.negate ? -a.scale_log2 : a.scale_log2;
     const RowInfo& info = (reinterpret_cast<const RowInfo*>(a.row_info) + (long long)bh * ((a.M + 31) / 32))[mc >> 5];
     const int lo = m < a.M ? info.lo[mc & 31] : 0, hi = m < a.M ? info.hi[mc & 31] : 0;
@@ -298,9 +300,10 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
     __shared__ __align__(16) float smem[2 * TILE];
     __shared__ RowInfo ri;
     const int tiles = (a.Sk + 127) / 128;
-    const int item = dense_item(a.B * a.Hkv * tiles);
-    if (item < 0) return;
-    const int tile = item % tiles, bh = item / tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+    const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
+    if (piece.rank < 0) return;
+    const DenseTask task = dense_task(piece.rank, a.splits, tiles, a.order_k);
+    const int tile = task.tile, b = task.b, hk = piece.head, bh = b * a.Hkv + hk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
     const int k0 = tile * 128, kw = k0 + wave * 32, key = kw + l32;
     const float scl = a.negate ? -a.scale_log2 : a.scale_log2;
@@ -316,27 +319,11 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
     unsigned found = 0;
     Stage<D, 256> sq, so;
     uint32_t si = 0;                                         // the thread's word of the row information
-    int window = 0;
-    unsigned long long pending = 0;
-    auto look = [&]() {
-        const int c = window + lane;
-        const int4 r = c < n_chunks ? bounds[c] : make_int4(INT32_MAX, 0, 0, 0);
-        pending = __builtin_amdgcn_ballot_w64(r.x < k0 + 128 && r.y > k0);
-    };
-    auto next_chunk = [&]() {
-        while (pending == 0) {
-            window += 64;
-            if (window >= n_chunks) return -1;
-            look();
-        }
-        const int i = __builtin_ctzll(pending);
-        pending &= pending - 1;
-        return window + i;
-    };
+    ChunkWalk walk(bounds, n_chunks, k0, k0 + 128, lane, task.split, a.splits);
     auto fetch = [&](int c) {
         auto row = [&](const TensorView& t) {
             return [&, c](int r) {
-                const int m = min(c * 32 + r, a.M - 1), q = m / a.G;
+                const int m = min(c * 32 + r, a.M - 1), q = query_of(a, m);
                 return row_ptr(t, b, q, hk * a.G + (m - q * a.G), 4);
             };
         };
@@ -344,19 +331,17 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
         so.load(row(a.dO));
         si = reinterpret_cast<const uint32_t*>(info + c)[tid];
     };
-    look();
-    int c = next_chunk();
+    int c = walk.next();
     if (c >= 0) fetch(c);
     while (c >= 0) {
-        const int4 bd = bounds[c];
+        const int all_lo = walk.all_lo, all_hi = walk.all_hi;
         __syncthreads();
         sq.store(smem);
         so.store(smem + TILE);
         reinterpret_cast<uint32_t*>(&ri)[tid] = si;
         __syncthreads();
-        c = next_chunk();
+        c = walk.next();
         if (c >= 0) fetch(c);
-        const int all_lo = __builtin_amdgcn_readfirstlane(bd.z), all_hi = __builtin_amdgcn_readfirstlane(bd.w);
         const bool masked = kw < all_lo || kw + 32 > all_hi;
         f32x16_t s = over_channels<D>(smem, kf, zero16, l32, hf), dp;
 #pragma unroll
@@ -369,8 +354,7 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
             pair_gradient<CAP>(a, s[v], scl, BIAS ? ri.slope2[r] * fabsf((float)(ri.pos[r] - key)) : 0.f, ri.lse2[r], dp[v], p, dz);
             if (masked) {
                 const bool reads = key >= ri.lo[r] && key < ri.hi[r];
-                // (a row of dO that is not finite shows in delta; its values are taken out of the product below)
-                p = !reads ? 0.f : fabsf(ri.ndelta[r]) < INFINITY ? p : NAN;
+                p = reads ? p : 0.f;
                 dz = reads ? dz : 0.f;
             }
             s[v] = p;
@@ -379,7 +363,12 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
         over_rows<D>(smem + TILE, s, dv, l32, hf, masked, found);
         over_rows<D>(smem, dp, dk, l32, hf, masked, found);
     }
-    if (key < a.Sk) {
+    if (key < a.Sk && a.splits > 1) {                        // this split's sums, added up by dense_sum_kernel
+        const long long n = (long long)a.B * a.Hkv * a.Sk;
+        float* dst = a.part_o + (2 * task.split * n + (long long)bh * a.Sk + key) * D;
+        store_row<D>((char*)dst, dk, a.scale, hf);
+        store_row<D>((char*)(dst + n * D), dv, 1.f, hf);
+    } else if (key < a.Sk) {
         store_row<D>(const_cast<char*>(row_ptr(a.dK, b, key, hk, 4)), dk, a.scale, hf);
         store_row<D>(const_cast<char*>(row_ptr(a.dV, b, key, hk, 4)), dv, 1.f, hf);
     }
@@ -395,14 +384,14 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
 
 template <int D, int NW>
 void launch_fwd(bool cap, hipStream_t st, const DenseArgs& a) {
-    const dim3 grid(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.M, 32 * NW) * a.splits)), block(64 * NW);
+    const dim3 grid(dense_grid((int64_t)a.B * ceil_div64(a.M, 32 * NW) * a.splits, a.Hkv)), block(64 * NW);
 #define LAUNCH(CAP, BIAS) dense_fwd_f32_kernel<D, NW, CAP, BIAS><<<grid, block, 0, st>>>(a)
     BY_SCORES(LAUNCH);
 #undef LAUNCH
 }
 template <int D>
 void launch_bwd(bool cap, hipStream_t st, const DenseArgs& a) {
-    const dim3 gq(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.M, 128))), gk(dense_grid((int64_t)a.B * a.Hkv * ceil_div64(a.Sk, 128))), block(256);
+    const dim3 gq(dense_grid((int64_t)a.B * ceil_div64(a.M, 128), a.Hkv)), gk(dense_grid((int64_t)a.B * ceil_div64(a.Sk, 128) * a.splits, a.Hkv)), block(256);
 #define LAUNCH(CAP, BIAS)                                            \
     do {                                                             \
         dense_dq_f32_kernel<D, CAP, BIAS><<<gq, block, 0, st>>>(a);  \
