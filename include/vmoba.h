@@ -318,8 +318,8 @@ size_t vmoba_rmsnorm_workspace_bytes(int B, int Hh, int64_t S, int D);
  *  x, residual  float32 or bfloat16, one dtype; residual may be null
  *  total        t, the same dtype; needed with a residual, null without
  *  weight       [D], weight_dtype float32 or bfloat16; null: ones
- *  y            the same dtype, or VMOBA_F8E4M3 with y_scale: then y holds round(t * inv * weight / y_scale), y_scale = the row's largest
- *               magnitude / 448 (1 for a row of zeros).  The quotient is taken in float32 and rounded once, to nearest even
+ *  y            the same dtype, or VMOBA_F8E4M3 with y_scale: then y holds round(t * inv * weight * (448 / m)), m the row's largest
+ *               magnitude of t * inv * weight, to nearest even, and y_scale = m / 448, so that y * y_scale is the row (a row of zeros: scale 1)
  *  y_scale      float32 [B, S, Hh], with VMOBA_F8E4M3 alone
  *  inv_rms      optional float32 [B, S, Hh]: inv, which the backward call reads
  *  Any strides and element-aligned addresses with contiguous channels; 1 <= D <= 16384.  An output may lie exactly on an input (same address

@@ -5,6 +5,7 @@ in the library's HIP kernels.  There is no fallback: if the library is missing, 
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 import struct
@@ -283,30 +284,37 @@ def vmoba_attn_bwd(B, Hh, S, D, n_blocks, blk_off, Qp, Kp, Vp, O, LSE, dO, blk_p
 
 
 # ------------------------------------------------------------------------------- around the sparse layer: positions, norms, dense attention
-def _on_device(**tensors):
+# A call on a few tokens is bound by the host: checks are comparisons on what a tensor hands out at once.
+def _on_device(*tensors):
     """The kernels run on the current device's stream: every tensor (None: left out) has to lie there."""
-    here = -1
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if t.is_cuda and here < 0:
-            here = _device() if _device else torch.cuda.current_device()
-        if not t.is_cuda or t.get_device() != here:
-            raise ValueError(f"{name} lies on {t.device}, not on the current GPU")
+    here = -2
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at != here:
+                if here == -2 and at >= 0:
+                    here = _device() if _device else torch.cuda.current_device()
+                if at != here:
+                    raise ValueError(f"a tensor of shape {tuple(t.shape)} lies on {t.device}, not on the current GPU")
 
 
-def _shaped(**tensors):
-    """name = (tensor or None, expected shape)"""
-    for name, (t, shape) in tensors.items():
-        if t is not None and tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
+def _shaped(name, t, shape):
+    if t is not None and t.shape != shape:
+        raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
 
 
 def _packed_array(t, name, dtype):
-    """A contiguous array of `dtype`, or None."""
-    if t is not None and (t.dtype != dtype or not t.is_contiguous()):
+    """Address of a contiguous array of `dtype`, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} has to be a contiguous {dtype} tensor")
-    return None if t is None else t.data_ptr()
+    return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=256)
+def _int_array(values):
+    return (C.c_int32 * max(1, len(values)))(*values)
 
 
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
@@ -316,9 +324,9 @@ VMOBA_F8E4M3 = 2
 
 def vmoba_rope_freqs(dims, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, train_len=0):
     """dims: channels rotated per axis.  Returns (float64 CPU tensor [sum(dims) / 2], mscale)."""
-    n = len(dims)
-    freqs, m = torch.empty(max(1, sum(int(d) for d in dims) // 2), dtype=torch.float64), C.c_float(0.0)
-    _check("vmoba_rope_freqs", lib().vmoba_rope_freqs(n, (C.c_int32 * max(1, n))(*dims), float(base), int(scaling), float(factor), int(train_len),
+    dims = tuple(int(d) for d in dims)
+    freqs, m = torch.empty(max(1, sum(dims) // 2), dtype=torch.float64), C.c_float(0.0)
+    _check("vmoba_rope_freqs", lib().vmoba_rope_freqs(len(dims), _int_array(dims), float(base), int(scaling), float(factor), int(train_len),
                                                       freqs.data_ptr(), C.byref(m)))
     return freqs, m.value
 
@@ -326,23 +334,23 @@ def vmoba_rope_freqs(dims, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, train_l
 def vmoba_rope(B, S, D, ins, outs, freqs, dims, layout=ROPE_HALF, inverse=False, mscale=1.0, grid=None, first=0, positions=None, stream=None):
     """ins / outs: lists of (b, s, h, d) views, each with its own number of heads; freqs: float64 [sum(dims) / 2] on the device; grid: (T, H, W);
     positions: int32 [B or 1, S, len(dims)]."""
-    n, axes = len(ins), len(dims)
+    n, dims = len(ins), tuple(dims)
     if len(outs) != n:
         raise ValueError("as many outputs as inputs")
-    for i, (x, y) in enumerate(zip(ins, outs)):
-        _on_device(**{f"ins[{i}]": x, f"outs[{i}]": y})
-        if x.dim() != 4:
-            raise ValueError("tensors are (b, s, h, d) views")
-        _shaped(**{f"ins[{i}]": (x, (B, S, x.shape[2], D)), f"outs[{i}]": (y, x.shape)})
-    _on_device(freqs=freqs, positions=positions)
-    _shaped(freqs=(freqs, (sum(dims) // 2,)))
-    shared = positions is not None and positions.dim() == 3 and positions.shape[0] == 1
-    _shaped(positions=(positions, (1 if shared else B, S, axes)))
-    g = make_grid(*grid) if grid is not None else None
-    rc = lib().vmoba_rope(B, S, D, n, (C.c_int32 * max(1, n))(*[x.shape[2] for x in ins]), b"".join(map(_desc, ins)), b"".join(map(_desc, outs)),
-                          _packed_array(freqs, "freqs", torch.float64), axes, (C.c_int32 * max(1, axes))(*dims), int(layout), int(inverse),
-                          float(mscale), g, int(first), _packed_array(positions, "positions", torch.int32), 0 if shared else S * axes,
-                          _stream(stream))
+    _on_device(freqs, positions, *ins, *outs)
+    heads = []
+    for x, y in zip(ins, outs):
+        shape = x.shape
+        if len(shape) != 4 or shape[0] != B or shape[1] != S or shape[3] != D or y.shape != shape:
+            raise ValueError(f"inputs and outputs have the shapes {tuple(shape)} and {tuple(y.shape)}, not [{B}, {S}, heads, {D}]")
+        heads.append(shape[2])
+    _shaped("freqs", freqs, (sum(dims) // 2,))
+    shared = positions is not None and positions.shape[0] == 1
+    _shaped("positions", positions, (1 if shared else B, S, len(dims)))
+    rc = lib().vmoba_rope(B, S, D, n, _int_array(tuple(heads)), b"".join(map(_desc, ins)), b"".join(map(_desc, outs)),
+                          _packed_array(freqs, "freqs", torch.float64), len(dims), _int_array(dims), int(layout), int(inverse),
+                          mscale, None if grid is None else make_grid(*grid), first, _packed_array(positions, "positions", torch.int32),
+                          0 if shared else S * len(dims), _stream(stream))
     _check("vmoba_rope", rc)
 
 
@@ -353,43 +361,45 @@ def vmoba_rmsnorm_workspace_bytes(B, Hh, S, D) -> int:
 def _weight(w, D):
     if w is None:
         return None, VMOBA_F32
-    _shaped(weight=(w, (D,)))
+    _shaped("weight", w, (D,))
     if not w.is_contiguous():
         raise ValueError("weight has to be contiguous")
     return w.data_ptr(), _dtype_code(w)
 
 
-def _norm_desc(t):
-    if t.dtype == torch.float8_e4m3fn:
-        return _desc_as(t, VMOBA_F8E4M3)
-    return _desc(t)
-
-
-def _desc_as(t, code):
+def _desc8(t):
+    """Descriptor of a tensor that may be float8_e4m3fn."""
+    if t.dtype != torch.float8_e4m3fn:
+        return _desc(t)
     strides = t.stride()
-    if len(strides) != 4 or strides[3] != 1:
-        raise ValueError("expect a (b, s, h, d) view with contiguous d")
-    return _pack_desc(t.data_ptr(), code, strides[0], strides[1], strides[2])
+    assert len(strides) == 4 and strides[3] == 1, "expect a (b, s, h, d) view with contiguous d"
+    return _pack_desc(t.data_ptr(), VMOBA_F8E4M3, strides[0], strides[1], strides[2])
 
 
 def vmoba_rmsnorm_fwd(B, Hh, S, D, x, residual, weight, eps, total, y, y_scale, inv_rms, stream=None):
     """x, residual, total, y: (b, s, h, d) views; y of x's type or float8_e4m3fn (then with y_scale [B, S, Hh]); residual and total, y_scale and
     inv_rms may be None."""
-    _on_device(x=x, residual=residual, weight=weight, total=total, y=y, y_scale=y_scale, inv_rms=inv_rms)
-    shape = (B, S, Hh, D)
-    _shaped(x=(x, shape), residual=(residual, shape), total=(total, shape), y=(y, shape), y_scale=(y_scale, shape[:3]), inv_rms=(inv_rms, shape[:3]))
+    _on_device(x, residual, weight, total, y, y_scale, inv_rms)
+    shape, rows = (B, S, Hh, D), (B, S, Hh)
+    for name, t in (("x", x), ("residual", residual), ("total", total), ("y", y)):
+        _shaped(name, t, shape)
+    _shaped("y_scale", y_scale, rows)
+    _shaped("inv_rms", inv_rms, rows)
     w, code = _weight(weight, D)
-    rc = lib().vmoba_rmsnorm_fwd(B, Hh, S, D, _desc(x), None if residual is None else _desc(residual), w, code, float(eps),
-                                 None if total is None else _desc(total), _norm_desc(y), _packed_array(y_scale, "y_scale", torch.float32),
+    rc = lib().vmoba_rmsnorm_fwd(B, Hh, S, D, _desc(x), None if residual is None else _desc(residual), w, code, eps,
+                                 None if total is None else _desc(total), _desc8(y), _packed_array(y_scale, "y_scale", torch.float32),
                                  _packed_array(inv_rms, "inv_rms", torch.float32), _stream(stream))
     _check("vmoba_rmsnorm_fwd", rc)
 
 
 def vmoba_rmsnorm_bwd(B, Hh, S, D, x, weight, inv_rms, dy, dtotal, dx, dweight, workspace, stream=None):
     """x: what was normalised (the forward call's total, if there was a residual).  dtotal and dweight (then also workspace) may be None."""
-    _on_device(x=x, weight=weight, inv_rms=inv_rms, dy=dy, dtotal=dtotal, dx=dx, dweight=dweight, workspace=workspace)
+    _on_device(x, weight, inv_rms, dy, dtotal, dx, dweight, workspace)
     shape = (B, S, Hh, D)
-    _shaped(x=(x, shape), inv_rms=(inv_rms, shape[:3]), dy=(dy, shape), dtotal=(dtotal, shape), dx=(dx, shape), dweight=(dweight, (D,)))
+    for name, t in (("x", x), ("dy", dy), ("dtotal", dtotal), ("dx", dx)):
+        _shaped(name, t, shape)
+    _shaped("inv_rms", inv_rms, shape[:3])
+    _shaped("dweight", dweight, (D,))
     w, code = _weight(weight, D)
     rc = lib().vmoba_rmsnorm_bwd(B, Hh, S, D, _desc(x), w, code, _packed_array(inv_rms, "inv_rms", torch.float32), _desc(dy),
                                  None if dtotal is None else _desc(dtotal), _desc(dx), _packed_array(dweight, "dweight", torch.float32),
@@ -399,15 +409,16 @@ def vmoba_rmsnorm_bwd(B, Hh, S, D, x, weight, inv_rms, dy, dtotal, dx, dweight, 
 
 def vmoba_key_ranges(B, Sq, Sk, key_lo, key_hi, doc_off=None, prefix=None, causal=False, q_pos=None, q_first=0, stream=None):
     """key_lo, key_hi: int32 [B, Sq]; doc_off: int32 [B or 1, documents + 1]; prefix: int32 [B or 1, documents]; q_pos: int32 [B, Sq]."""
-    _on_device(key_lo=key_lo, key_hi=key_hi, doc_off=doc_off, prefix=prefix, q_pos=q_pos)
+    _on_device(key_lo, key_hi, doc_off, prefix, q_pos)
     docs = 1 if doc_off is None else doc_off.shape[-1] - 1
-    rows = lambda t: 1 if t is not None and t.shape[0] == 1 else B            # noqa: E731
-    _shaped(key_lo=(key_lo, (B, Sq)), key_hi=(key_hi, (B, Sq)), doc_off=(doc_off, (rows(doc_off), docs + 1)), prefix=(prefix, (rows(prefix), docs)),
-            q_pos=(q_pos, (B, Sq)))
+    doc_rows, prefix_rows = (1 if t is not None and t.shape[0] == 1 else B for t in (doc_off, prefix))
+    for name, t, shape in (("key_lo", key_lo, (B, Sq)), ("key_hi", key_hi, (B, Sq)), ("q_pos", q_pos, (B, Sq)), ("doc_off", doc_off, (doc_rows, docs + 1)),
+                           ("prefix", prefix, (prefix_rows, docs))):
+        _shaped(name, t, shape)
     i32 = torch.int32
-    rc = lib().vmoba_key_ranges(B, Sq, Sk, _packed_array(doc_off, "doc_off", i32), 0 if rows(doc_off) == 1 else docs + 1, docs,
-                                _packed_array(prefix, "prefix", i32), 0 if rows(prefix) == 1 else docs, int(causal), _packed_array(q_pos, "q_pos", i32),
-                                int(q_first), _packed_array(key_lo, "key_lo", i32), _packed_array(key_hi, "key_hi", i32), _stream(stream))
+    rc = lib().vmoba_key_ranges(B, Sq, Sk, _packed_array(doc_off, "doc_off", i32), 0 if doc_rows == 1 else docs + 1, docs,
+                                _packed_array(prefix, "prefix", i32), 0 if prefix_rows == 1 else docs, int(causal), _packed_array(q_pos, "q_pos", i32),
+                                q_first, _packed_array(key_lo, "key_lo", i32), _packed_array(key_hi, "key_hi", i32), _stream(stream))
     _check("vmoba_key_ranges", rc)
 
 
@@ -416,19 +427,22 @@ def vmoba_dense_workspace_bytes(op, B, Hq, Hkv, Sq, Sk, D, dtype) -> int:
 
 
 def _scores(B, Hq, Sq, softmax_scale, cap, slopes, key_lo, key_hi, q_pos, q_first):
-    _on_device(slopes=slopes, key_lo=key_lo, key_hi=key_hi, q_pos=q_pos)
-    _shaped(slopes=(slopes, (Hq,)), key_lo=(key_lo, (B, Sq)), key_hi=(key_hi, (B, Sq)), q_pos=(q_pos, (B, Sq)))
+    _on_device(slopes, key_lo, key_hi, q_pos)
+    _shaped("slopes", slopes, (Hq,))
+    for name, t in (("key_lo", key_lo), ("key_hi", key_hi), ("q_pos", q_pos)):
+        _shaped(name, t, (B, Sq))
     i32 = torch.int32
-    return vmoba_scores(float(softmax_scale), float(cap), _packed_array(slopes, "slopes", torch.float32), _packed_array(key_lo, "key_lo", i32),
-                        _packed_array(key_hi, "key_hi", i32), _packed_array(q_pos, "q_pos", i32), int(q_first))
+    return vmoba_scores(softmax_scale, cap, _packed_array(slopes, "slopes", torch.float32), _packed_array(key_lo, "key_lo", i32),
+                        _packed_array(key_hi, "key_hi", i32), _packed_array(q_pos, "q_pos", i32), q_first)
 
 
 def vmoba_dense_fwd(B, Hq, Hkv, Sq, Sk, D, Q, K, V, O, LSE, workspace, softmax_scale, cap=0.0, slopes=None, key_lo=None, key_hi=None, q_pos=None,
                     q_first=0, stream=None):
     """Q, O: (b, s, h, d) views of Hq heads, K, V of Hkv; LSE: float32 [B, Hq, Sq]."""
-    _on_device(Q=Q, K=K, V=V, O=O, LSE=LSE, workspace=workspace)
+    _on_device(Q, K, V, O, LSE, workspace)
     q, k = (B, Sq, Hq, D), (B, Sk, Hkv, D)
-    _shaped(Q=(Q, q), K=(K, k), V=(V, k), O=(O, q), LSE=(LSE, (B, Hq, Sq)))
+    for name, t, shape in (("Q", Q, q), ("K", K, k), ("V", V, k), ("O", O, q), ("LSE", LSE, (B, Hq, Sq))):
+        _shaped(name, t, shape)
     how = _scores(B, Hq, Sq, softmax_scale, cap, slopes, key_lo, key_hi, q_pos, q_first)
     rc = lib().vmoba_dense_fwd(B, Hq, Hkv, Sq, Sk, D, _desc(Q), _desc(K), _desc(V), how, _desc(O), _packed_array(LSE, "LSE", torch.float32),
                                _ptr(workspace), workspace.nbytes, _stream(stream))
@@ -437,9 +451,11 @@ def vmoba_dense_fwd(B, Hq, Hkv, Sq, Sk, D, Q, K, V, O, LSE, workspace, softmax_s
 
 def vmoba_dense_bwd(B, Hq, Hkv, Sq, Sk, D, Q, K, V, O, LSE, dO, dQ, dK, dV, workspace, softmax_scale, cap=0.0, slopes=None, key_lo=None,
                     key_hi=None, q_pos=None, q_first=0, stream=None):
-    _on_device(Q=Q, K=K, V=V, O=O, LSE=LSE, dO=dO, dQ=dQ, dK=dK, dV=dV, workspace=workspace)
+    _on_device(Q, K, V, O, LSE, dO, dQ, dK, dV, workspace)
     q, k = (B, Sq, Hq, D), (B, Sk, Hkv, D)
-    _shaped(Q=(Q, q), K=(K, k), V=(V, k), O=(O, q), LSE=(LSE, (B, Hq, Sq)), dO=(dO, q), dQ=(dQ, q), dK=(dK, k), dV=(dV, k))
+    for name, t, shape in (("Q", Q, q), ("K", K, k), ("V", V, k), ("O", O, q), ("LSE", LSE, (B, Hq, Sq)), ("dO", dO, q), ("dQ", dQ, q), ("dK", dK, k),
+                           ("dV", dV, k)):
+        _shaped(name, t, shape)
     how = _scores(B, Hq, Sq, softmax_scale, cap, slopes, key_lo, key_hi, q_pos, q_first)
     rc = lib().vmoba_dense_bwd(B, Hq, Hkv, Sq, Sk, D, _desc(Q), _desc(K), _desc(V), how, _desc(O), _packed_array(LSE, "LSE", torch.float32), _desc(dO),
                                _desc(dQ), _desc(dK), _desc(dV), _ptr(workspace), workspace.nbytes, _stream(stream))

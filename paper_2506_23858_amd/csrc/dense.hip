@@ -108,14 +108,15 @@ __global__ __launch_bounds__(256) void dense_sum_kernel(DenseArgs a) {
 
 // Tiles in order of falling cost, so that the long ones do not begin when the others are done.  One workgroup for the row tiles (cost: keys between the first and the
 // last that its rows read; forward: that its first, middle and last row read, an estimate that costs three look-ups) and, in a
-// backward call, a second one for the key tiles (cost: chunks of 32 rows that read one of its keys).  Costs are sorted into 64 classes.
+// backward call, a second one for the key tiles (cost: chunks of 32 rows that read one of its keys).  Tiles with masks count more.  Costs are sorted into 64 classes.
 struct OrderArgs { int *order_q, *cost_q, *order_k, *cost_k; int rows_per_tile; };
 __global__ __launch_bounds__(1024) void dense_order_kernel(DenseArgs a, OrderArgs o) {
     __shared__ int classes[64], top;
     const bool keys = blockIdx.x == 1;
     const int tiles = keys ? (a.Sk + DENSE_TILE_ROWS - 1) / DENSE_TILE_ROWS : (a.M + o.rows_per_tile - 1) / o.rows_per_tile, n = a.B * tiles, t = threadIdx.x;
     const int n_chunks = (a.M + 31) / 32;
-    int *cost = keys ? o.cost_k : o.cost_q, *order = keys ? o.order_k : o.order_q;
+    __shared__ int near[8192];                               // costs of as many tiles
+    int *cost = n <= 8192 ? near : keys ? o.cost_k : o.cost_q, *order = keys ? o.order_k : o.order_q;
     if (t < 64) classes[t] = 0;
     if (t == 0) top = 1;
     if (keys) {                                              // +1 where a chunk's keys begin, -1 behind their end; then running sums
@@ -126,8 +127,13 @@ __global__ __launch_bounds__(1024) void dense_order_kernel(DenseArgs a, OrderArg
             const int4 r = a.row_bounds[(long long)b * a.Hkv * n_chunks + (i - b * n_chunks)];
             if (r.x >= r.y) continue;
             const int first = r.x / DENSE_TILE_ROWS, last = (r.y - 1) / DENSE_TILE_ROWS;
-            atomicAdd(cost + b * tiles + first, 1);
-            if (last + 1 < tiles) atomicSub(cost + b * tiles + last + 1, 1);
+            auto add = [&](int from, int to) {
+                atomicAdd(cost + b * tiles + from, 1);
+                if (to + 1 < tiles) atomicSub(cost + b * tiles + to + 1, 1);
+            };
+            add(first, last);
+            if (r.x % DENSE_TILE_ROWS) add(first, first);    // (a tile that is read in part counts twice: masks)
+            if (r.y % DENSE_TILE_ROWS) add(last, last);
         }
         __syncthreads();
         for (int b = t >> 6; b < a.B; b += 16) {             // a wavefront per batch element
@@ -148,12 +154,14 @@ __global__ __launch_bounds__(1024) void dense_order_kernel(DenseArgs a, OrderArg
     } else {
         for (int i = t; i < n; i += 1024) {
             const int b = i / tiles, m0 = (i - b * tiles) * o.rows_per_tile, m1 = min(m0 + o.rows_per_tile, a.M) - 1;
-            int first = INT32_MAX, end = 0;
+            int first = INT32_MAX, end = 0, all_first = 0, all_end = INT32_MAX;
             if (o.cost_k) {
                 for (int c = m0 >> 5; c <= m1 >> 5; ++c) {
                     const int4 r = a.row_bounds[(long long)b * a.Hkv * n_chunks + c];
                     first = min(first, r.x);
                     end = max(end, r.y);
+                    all_first = max(all_first, r.z);
+                    all_end = min(all_end, r.w);
                 }
             } else {
 #pragma unroll
@@ -162,10 +170,13 @@ __global__ __launch_bounds__(1024) void dense_order_kernel(DenseArgs a, OrderArg
                     if (r.x < r.y) {
                         first = min(first, r.x);
                         end = max(end, r.y);
+                        all_first = max(all_first, r.x);
+                        all_end = min(all_end, r.y);
                     }
                 }
             }
-            cost[i] = max(end - first, 0) / 32;
+            const int keys_read = max(end - first, 0);
+            cost[i] = (keys_read + (first != all_first || end != all_end ? keys_read / 2 : 0)) / 32;      // (rows of several ranges: masks)
         }
     }
     __syncthreads();

@@ -3,8 +3,10 @@
 // them (S, dP, dV, dK: four).  Seven products for the five that a single pass with dQ in atomics would need.
 //
 // dz = P (dP - delta) (1 - tanh^2), rounded to bfloat16 for the products that follow (relative error 2^-9 a value, like P's).
-// Masked pairs: their scores are replaced (-inf, or 0 with an infinite log-sum-exp), so P and dz are 0, and tiles with masked pairs lose their values that are not finite in LDS before
-// they are multiplied -- 0 times infinity is no number.  A pair that does read such a value has a log-sum-exp or a delta that is not finite, and gives NaN.
+// Masked pairs: their scores are replaced (-inf, or 0 with an infinite log-sum-exp), so P and dz are 0.  A masked value that is not finite would still spoil a sum -- 0 times
+// infinity is no number --, so tiles that pass the last key or hold rows without keys lose such values in LDS before they are multiplied, and a
+// workgroup whose sums end up not finite starts again with all tiles cleaned so.  A pair that does read such a value has a log-sum-exp or a delta that is not
+// finite, and gives NaN.
 #include "dense_common.h"
 
 namespace {
@@ -61,10 +63,12 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
         ndl[t] = f32x4_t{d, d, d, d};
         slope2[t] = BIAS ? r.slope2[mc & 31] : 0.f;
         row_pos[t] = BIAS ? r.pos[mc & 31] : 0;
+        const bool some = lo[t] < hi[t];            // (a row without keys: a query of zeros, weights of 0 by its log-sum-exp)
         const char *p = row_ptr(a.Q, b, q, h, 2) + g * 16, *p2 = row_ptr(a.dO, b, q, h, 2) + g * 16;
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
-            qf[t][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(p + ks * 64) ^ a.negate);
+            const u32x4_t x = *reinterpret_cast<const u32x4_t*>(p + ks * 64) ^ a.negate;
+            qf[t][ks] = __builtin_bit_cast(bf16x8_t, some ? x : u32x4_t{0u, 0u, 0u, 0u});
             unsigned unused = 0;      // (what was not finite shows in the row's log-sum-exp, see dense_rows_kernel)
             dof[t][ks] = finite_only(*reinterpret_cast<const bf16x8_t*>(p2 + ks * 64), unused);
         }
@@ -75,8 +79,9 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
         const bool some = lo[t] < hi[t];
         any_lo = min(any_lo, some ? lo[t] : INT32_MAX);
         any_hi = max(any_hi, some ? hi[t] : 0);
-        all_lo = max(all_lo, some ? lo[t] : INT32_MAX);
-        all_hi = min(all_hi, some ? hi[t] : 0);
+        all_lo = max(all_lo, some ? lo[t] : 0);
+        all_hi = min(all_hi, some ? hi[t] : INT32_MAX);
+        if (m0 + 16 * t + l16 >= a.M) lse2[t] = INFINITY;
     }
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) {
@@ -87,21 +92,20 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     }
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
     all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-    int tile_lo = all_lo, tile_hi = all_hi;     // keys that all rows of the workgroup read
-    {
-        int4* w = reinterpret_cast<int4*>(smem + 2 * BUF);
-        if (lane == 0) w[wave] = make_int4(any_lo, any_hi, all_lo, all_hi);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            any_lo = min(any_lo, w[i].x);
-            any_hi = max(any_hi, w[i].y);
-            tile_lo = max(tile_lo, w[i].z);
-            tile_hi = min(tile_hi, w[i].w);
-        }
-        tile_lo = __builtin_amdgcn_readfirstlane(tile_lo);
-        tile_hi = __builtin_amdgcn_readfirstlane(tile_hi);
+    const int wave_lo = __builtin_amdgcn_readfirstlane(any_lo), wave_hi = __builtin_amdgcn_readfirstlane(any_hi);
+    int* const words = reinterpret_cast<int*>(smem + 2 * BUF);
+    if (lane == 0) {
+        words[wave] = any_lo;
+        words[4 + wave] = any_hi;
     }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        any_lo = min(any_lo, words[i]);
+        any_hi = max(any_hi, words[4 + i]);
+    }
+    __syncthreads();
+    if (tid == 0) words[0] = 0;                 // from here on: whether a sum is not finite
     int k_first = __builtin_amdgcn_readfirstlane(any_lo), k_end = __builtin_amdgcn_readfirstlane(any_hi);
     if (k_first >= k_end) k_first = k_end = 0;
     const int n_chunks = (k_end - k_first + KC - 1) / KC;
@@ -122,8 +126,7 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     };
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
     f32x4_t acc[CT][2];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) acc[ct][0] = acc[ct][1] = zero4;
+    bool careful = false;                       // every chunk is cleaned and masked
     const uint32_t rlane = TL::row_lane(lane, 0), tlane = TL::tr_lane(lane, 0);
     uint32_t rows0 = 0, cols0 = 0;              // lane addresses in the current chunk's buffer
 
@@ -131,20 +134,22 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     // the same, the third product over the channel tiles.  Operands pass through a ring, fetched AHEAD units before use; weights are computed
     // between the matrix instructions, those of the first 16 keys from the middle of the first phase on.  Fences keep that order.
     constexpr int NP = 2 * KSTEPS, NSEQ = 3 * NP, AHEAD = 3, RING = AHEAD + 1;
-    static_assert(NP == CT && NSEQ % RING == 0, "as many units in each phase; the second group continues the ring where the first one left it");
-    auto fetch = [&](int mt, int n) -> bf16x8_t {      // operand of unit n of group mt (n past the end: next group)
-        if (n >= NSEQ) { mt += 1; n -= NSEQ; }
+    static_assert(NP == CT, "as many units in each phase");
+    auto fetch = [&](int mt, int n) -> bf16x8_t {      // operand of unit n of group mt
         if (n < NP) return TL::rows(smem + mt * HB, rows0, n / KSTEPS, n % KSTEPS);
         if (n < 2 * NP) return TL::rows(smem + (2 + mt) * HB, rows0, (n - NP) / KSTEPS, n % KSTEPS);
         return TL::transposed(smem + mt * HB, cols0, n - 2 * NP);
     };
+again:
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) acc[ct][0] = acc[ct][1] = zero4;
     if (n_chunks > 0) request(0);
     VMOBA_WAIT_VMCNT(0);
     __syncthreads();
     for (int c = 0; c < n_chunks; ++c) {
         const uint32_t buf = (uint32_t)(c & 1) * BUF;
         const int kc = k_first + c * KC;
-        if (__builtin_expect(kc < tile_lo || kc + KC > tile_hi, 0)) {
+        if (__builtin_expect(careful || kc + KC > k_end, 0)) {
             clean_tile(smem + buf, BUF, 256);
             __syncthreads();
         }
@@ -153,12 +158,10 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
         cols0 = tlane + buf;
         bf16x8_t op[RING];
 #pragma unroll
-        for (int n = 0; n < RING; ++n) op[n] = fetch(0, n < AHEAD ? n : 0);
-#pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
             const int kb = kc + mt * 32;
-            if (kb < k_end) {
-                const bool masked = kb < all_lo || kb + 32 > all_hi;
+            if (kb + 32 > wave_lo && kb < wave_hi) {      // (keys that one of the wavefront's rows reads)
+                const bool masked = careful || kb < all_lo || kb + 32 > all_hi;
                 f32x4_t s[2][2], dp[2][2];            // [16 keys][16 rows]: value i is key 16 * kt + 4 * g + i
                 bf16x8_t ds[2];
                 float rel[2];
@@ -179,9 +182,10 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
                     s[kt][t][i] = d;
                 };
 #pragma unroll
+                for (int n = 0; n < RING; ++n) op[n] = fetch(mt, n < AHEAD ? n : 0);
+#pragma unroll
                 for (int n = 0; n < NSEQ; ++n) {
-                    // (the group after the second one waits for the next chunk)
-                    if (n + AHEAD < NSEQ || mt == 0) op[(n + AHEAD) % RING] = fetch(mt, n + AHEAD);
+                    if (n + AHEAD < NSEQ) op[(n + AHEAD) % RING] = fetch(mt, n + AHEAD);
                     const int m = n % NP, kt = m / KSTEPS, ks = m % KSTEPS;
                     if ((n == KSTEPS + 1 || n == NP) && __builtin_expect(masked, 0)) {      // the scores of the first, of the second 16 keys are complete
                         const int half = n == NP ? 1 : 0;
@@ -226,6 +230,21 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
         VMOBA_WAIT_VMCNT(0);
         __syncthreads();
     }
+    if (!careful) {
+        float z = 0.f;                          // NaN if a sum is not finite
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z = fmaf(acc[ct][t][i], 0.f, z);
+        if (__builtin_expect(z != 0.f, 0)) words[0] = 1;
+        __syncthreads();
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(words[0]) != 0, 0)) {
+            careful = true;
+            goto again;
+        }
+    }
     char* mine = smem + wave * 32 * OPITCH;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -267,7 +286,7 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
     constexpr int IPW = 32 / RPI / 4;
     constexpr int OPITCH = D * 2 + 16;
     static_assert(IPW >= 1 && IPW % TL::NPC == 0 && 4 * 32 * OPITCH <= B0 + 2 * BUF, "requests, rows on their way out");
-    __shared__ __align__(1024) char smem[B0 + 2 * BUF];
+    __shared__ __align__(1024) char smem[B0 + 2 * BUF + 16];
 
     const int tiles = (a.Sk + 127) / 128;
     const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
@@ -311,8 +330,9 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
 
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
     f32x4_t dv[CT][2], dk[CT][2];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) dv[ct][0] = dv[ct][1] = dk[ct][0] = dk[ct][1] = zero4;
+    bool careful = false;                                // every chunk is cleaned and masked
+    int* const words = reinterpret_cast<int*>(smem + B0 + 2 * BUF);
+    if (tid == 0) words[0] = 0;                          // whether a sum is not finite
     const uint32_t rlane = TL::row_lane(lane, 0), tlane = TL::tr_lane(lane, 0);
 
     // A chunk is a sequence of units: S over (16 rows, k-step), one operand and two matrix instructions (one per 16 keys) each; dP over the k-steps, four operands (V of both key
@@ -320,6 +340,9 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
     // first phase and in the second one, dz in the third.
     constexpr int NP = 2 * KSTEPS;
     static_assert(NP == CT, "as many units in the first phase as in the last two");
+again:
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) dv[ct][0] = dv[ct][1] = dk[ct][0] = dk[ct][1] = zero4;
     int c = walk.next(), par = 0;
     if (c >= 0) request(c, 0);
     VMOBA_WAIT_VMCNT(0);
@@ -328,15 +351,21 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
     __syncthreads();
     while (c >= 0) {
         const int all_lo = walk.all_lo, all_hi = walk.all_hi;
+        const bool one_range = walk.any_lo == all_lo && walk.any_hi == all_hi;      // of all the chunk's rows
+        const bool none = kw >= walk.any_hi || kw + 32 <= walk.any_lo;              // of the wavefront's keys is read
         const uint32_t buf = B0 + (uint32_t)par * BUF;
         const RowInfo* ri = reinterpret_cast<const RowInfo*>(smem + buf + 2 * HB);
-        const bool masked = kw < all_lo || kw + 32 > all_hi;
-        if (__builtin_expect(k0 < all_lo || k0 + 128 > all_hi, 0)) {
+        const bool masked = careful || kw < all_lo || kw + 32 > all_hi;
+        if (__builtin_expect(careful || all_lo == INT32_MAX, 0)) {      // (a chunk with rows that read no key)
             clean_tile(smem + buf, 2 * HB, 256);
             __syncthreads();
         }
         const int c_next = walk.next();
         if (c_next >= 0) request(c_next, par ^ 1);
+        if (__builtin_expect(!none, 1)) {
+        bool reads[2];                                    // one range: whether the chunk's rows read the lane's keys
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) reads[kt] = kw + 16 * kt + l16 >= all_lo && kw + 16 * kt + l16 < all_hi;
         const uint32_t rows0 = rlane + buf, cols0 = tlane + buf, vrows0 = pinned(rlane) + (uint32_t)wave * HB;
         f32x4_t s[2][2], dp[2][2];                        // [16 rows][16 keys]: value i is row 16 * t + 4 * g + i
         unsigned pw[2][4];                                // P as packed pairs
@@ -347,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
             if (__builtin_expect(masked, 0)) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    if (key < ri->lo[r0 + e] || key >= ri->hi[r0 + e]) {
+                    if (one_range ? !reads[kt] : key < ri->lo[r0 + e] || key >= ri->hi[r0 + e]) {
                         s[t][kt][i0 + e] = 0.f;
                         l2[e] = INFINITY;
                     }
@@ -440,10 +469,27 @@ __global__ __launch_bounds__(256, 2) void dense_dkv_kernel(DenseArgs a) {
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        }
         VMOBA_WAIT_VMCNT(0);
         __syncthreads();
         c = c_next;
         par ^= 1;
+    }
+    if (!careful) {
+        float z = 0.f;                                    // NaN if a sum is not finite
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z = fmaf(dk[ct][kt][i], 0.f, fmaf(dv[ct][kt][i], 0.f, z));
+        if (__builtin_expect(z != 0.f, 0)) words[0] = 1;
+        __syncthreads();
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(words[0]) != 0, 0)) {
+            careful = true;
+            walk.window = -64;
+            goto again;
+        }
     }
     if (a.splits > 1) {                                   // this split's sums, added up by dense_sum_kernel
         const long long n = (long long)a.B * a.Hkv * a.Sk;

@@ -106,8 +106,8 @@ __device__ __forceinline__ bf16x8_t finite_only(bf16x8_t x, unsigned& found) {
     }
     return __builtin_bit_cast(bf16x8_t, w);
 }
-// The forward kernels' last step for a wavefront that met values of V that are not finite in groups of 32 keys with masked pairs, where they were
-// taken out of the product: the rows that do read such a key get weight times value added.  A rare path, one key at a time.  lo_a, hi_a, lse_a
+// The forward kernels' last step for a wavefront that met values of V that are not finite in groups of 32 keys where they were taken out of the product: those not
+// inside all_lo .. all_hi.  The rows that do read such a key get weight times value added.  A rare path, one key at a time.  lo_a, hi_a, lse_a
 // (base 2) are those of row m0 + lane % 16, _b of row m0 + 16 + lane % 16; part0: place of the split's first row.
 template <class T, int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void dense_repair(const DenseArgs& a, int b, int hk, int m0, int lane, long long part0, int k_first, int k_end, int all_lo,
@@ -164,7 +164,7 @@ struct ChunkWalk {
     int n, first, end, lane, split, splits, window = -64;
     unsigned long long pending = 0;
     int4 mine;
-    int all_lo, all_hi;      // of the chunk that next() returned: keys that all its rows read
+    int any_lo, any_hi, all_lo, all_hi;      // of the chunk that next() returned: keys that any of its rows, that all of them read
     __device__ __forceinline__ ChunkWalk(const int4* b, int chunks, int k0, int k1, int l, int s, int ss)
         : bounds(b), n(chunks), first(k0), end(k1), lane(l), split(s), splits(ss) {}
     __device__ __forceinline__ int next() {
@@ -177,6 +177,8 @@ struct ChunkWalk {
         }
         const int i = __builtin_ctzll(pending);
         pending &= pending - 1;
+        any_lo = __builtin_amdgcn_readlane(mine.x, i);
+        any_hi = __builtin_amdgcn_readlane(mine.y, i);
         all_lo = __builtin_amdgcn_readlane(mine.z, i);
         all_hi = __builtin_amdgcn_readlane(mine.w, i);
         return window + i;

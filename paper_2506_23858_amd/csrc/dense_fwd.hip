@@ -13,9 +13,10 @@
 // The running maximum is raised only when a score passes it by 2^8 (weights stay below 2^8), so a step mostly compares and does not rescale.
 // Weights are rounded to bfloat16 for the second product (relative error 2^-9 each, as the inputs'); their sum is that of the float32 values.
 //
-// Masks.  A row reads keys lo .. hi - 1.  A group that all of the wavefront's rows read whole takes no test.  In the others scores outside the range
-// are replaced by -inf, and values that are not finite by 0 in LDS -- weight 0 times infinity is no number --; if there were any, the rows
-// that do read them get weight times value added at the end (dense_repair).
+// Masks.  A row reads keys lo .. hi - 1.  A group that all of the wavefront's rows read whole takes no test; in the others scores outside the range
+// are replaced by -inf.  A masked value that is not finite would still spoil its row -- weight 0 times infinity is no number --, so the group that passes the
+// last key loses such values in LDS before it is multiplied, and a tile whose sums end up not finite is computed again with all groups
+// cleaned so; the rows that do read such values then get weight times value added (dense_repair).  Rows without keys take part with a query of zeros; their sums are dropped.
 //
 // NW = 4: 128 rows, two workgroups per compute unit.  NW = 1: up to 32 rows (single queries), where the keys' bytes are what counts.  With
 // few tiles the keys are split over `splits` workgroups, whose normalised rows and sums a second launch joins.
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
     constexpr int V0 = NR * SLOT;
     constexpr int OPITCH = D * 2 + 16;
     static_assert(UNITS == 2 * KSTEPS && IPW >= 1 && IPW % TL::NPC == 0, "units, requests");
-    __shared__ __align__(1024) char smem[2 * NR * SLOT + 16 * NW];
+    __shared__ __align__(1024) char smem[2 * NR * SLOT + 32];
     static_assert(NW * ROWS * OPITCH <= 2 * NR * SLOT, "the tile's rows on their way out");
 
     const int tiles = (a.M + ROWS * NW - 1) / (ROWS * NW);
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
     int lo[QT], hi[QT], row_pos[QT];
     float slope2[QT];
     bf16x8_t qf[QT][KSTEPS];
-    int any_lo = INT32_MAX, any_hi = 0, all_lo = 0, all_hi = INT32_MAX;      // keys of any row and of all; a row without keys makes every group a masked one
+    int any_lo = INT32_MAX, any_hi = 0, all_lo = 0, all_hi = INT32_MAX;      // keys of any row and of all (that have any)
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int m = m0 + 16 * t + l16, mc = min(m, a.M - 1), q = query_of(a, mc), h = hk * a.G + (mc - q * a.G);
@@ -73,14 +74,17 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
         hi[t] = m < a.M ? r.y : 0;
         slope2[t] = BIAS ? a.slopes[h] * DENSE_LOG2E : 0.f;
         row_pos[t] = BIAS ? dense_position(a, b, q) : 0;
+        const bool some = lo[t] < hi[t];
         const char* p = row_ptr(a.Q, b, q, h, 2) + g * 16;
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) qf[t][ks] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(p + ks * 64) ^ a.negate);
-        const bool some = lo[t] < hi[t];
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+            const u32x4_t x = *reinterpret_cast<const u32x4_t*>(p + ks * 64) ^ a.negate;
+            qf[t][ks] = __builtin_bit_cast(bf16x8_t, some ? x : u32x4_t{0u, 0u, 0u, 0u});
+        }
         any_lo = min(any_lo, some ? lo[t] : INT32_MAX);
         any_hi = max(any_hi, some ? hi[t] : 0);
-        all_lo = max(all_lo, some ? lo[t] : INT32_MAX);
-        all_hi = min(all_hi, some ? hi[t] : 0);
+        all_lo = max(all_lo, some ? lo[t] : 0);
+        all_hi = min(all_hi, some ? hi[t] : INT32_MAX);
     }
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) {
@@ -91,24 +95,22 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
     }
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
     all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-    int tile_lo = all_lo, tile_hi = all_hi;                  // keys that all rows of the workgroup read
-    int* const words = reinterpret_cast<int*>(smem + 2 * NR * SLOT);      // and, in word 0 later, whether a value was not finite
+    int* const words = reinterpret_cast<int*>(smem + 2 * NR * SLOT);
     if constexpr (NW > 1) {
-        if (lane == 0) *reinterpret_cast<int4*>(words + 4 * wave) = make_int4(any_lo, any_hi, all_lo, all_hi);
+        if (lane == 0) {
+            words[wave] = any_lo;
+            words[NW + wave] = any_hi;
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
-            const int4 x = *reinterpret_cast<const int4*>(words + 4 * i);
-            any_lo = min(any_lo, x.x);
-            any_hi = max(any_hi, x.y);
-            tile_lo = max(tile_lo, x.z);
-            tile_hi = min(tile_hi, x.w);
+            any_lo = min(any_lo, words[i]);
+            any_hi = max(any_hi, words[NW + i]);
         }
-        tile_lo = __builtin_amdgcn_readfirstlane(tile_lo);
-        tile_hi = __builtin_amdgcn_readfirstlane(tile_hi);
         __syncthreads();
     }
-    if (tid == 0) words[0] = 0;
+    // from here on: whether a value that was cleaned away was not finite, whether a sum is not
+    if (tid < 2) words[tid] = 0;
     int k_first = __builtin_amdgcn_readfirstlane(any_lo), k_end = __builtin_amdgcn_readfirstlane(any_hi);
     if (k_first >= k_end) k_first = k_end = 0;
     if (a.splits > 1) {                                      // this split's share of the tile's groups
@@ -117,25 +119,25 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
         k_end = min(k_end, k_first + s1 * GK);
         k_first += s0 * GK;
     }
-    tile_hi = min(tile_hi, k_end);
     all_hi = min(all_hi, k_end);
     const int n_groups = (k_end - k_first + GK - 1) / GK;
 
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
     f32x4_t oacc[CT][QT];
+    // m: what is subtracted from base-2 scores; limit: the (kept) score that raises it.  l: this lane's share of the row's sum
+    float m_run[QT], limit[QT], l_run[QT];
+    bool careful = false;                                    // every group is cleaned and masked
+again:
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int t = 0; t < QT; ++t) oacc[ct][t] = zero4;
-    // m: what is subtracted from base-2 scores; limit: the (kept) score that raises it.  l: this lane's share of the row's sum
-    float m_run[QT], limit[QT], l_run[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         m_run[t] = -3e38f;
         limit[t] = -INFINITY;
         l_run[t] = 0.f;
     }
-
     if (n_groups > 0) {
         const char *kbase = row_ptr(a.K, b, 0, hk, 2), *vbase = row_ptr(a.V, b, 0, hk, 2);
         const uint32_t kss = (uint32_t)(a.K.stride_s * 2), vss = (uint32_t)(a.V.stride_s * 2);
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
         // unit u of S^T: keys 16 * (u / KSTEPS), k-step u % KSTEPS; of the second product: channel tile u.  Ring places are constants in the steps
         auto readK = [&](int slot, int u) { return TL::rows(smem + slot * SLOT, rlane, 0, u / KSTEPS, u % KSTEPS); };
         auto readV = [&](int slot, int u) { return TL::transposed(smem + V0 + slot * SLOT, tlane, 0, u); };
-        // A group with masked pairs: its values that are not finite become 0 before anybody reads them
+        // A group's values that are not finite become 0 before anybody reads them
         auto clean_values = [&](int slot) {
             if (clean_tile(smem + V0 + slot * SLOT, SLOT, 64 * NW)) words[0] = 1;
             __builtin_amdgcn_s_waitcnt(0xC07F);
@@ -218,10 +220,10 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
             VMOBA_WAIT_VMCNT(2 * IPW);
             asm volatile("s_barrier" ::: "memory");
             const int kb = k_first + n * GK;
-            if (__builtin_expect(kb < tile_lo || kb + GK > tile_hi, 0)) clean_values(R);
+            if (__builtin_expect(careful || kb + GK > k_end, 0)) clean_values(R);
 #pragma unroll
             for (int v = 0; v < 4 * QT; ++v) keep_score(s, 1, v >> 2, v & 3, kb);
-            if (__builtin_expect(kb < all_lo || kb + GK > all_hi, 0)) {
+            if (__builtin_expect(careful || kb < all_lo || kb + GK > all_hi, 0)) {
 #pragma unroll
                 for (int t = 0; t < QT; ++t) {
                     const int first_key = lo[t] - kb - 4 * g, end = min(hi[t], k_end) - kb - 4 * g;
@@ -344,6 +346,21 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) oacc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pA[t], oacc[u][t], 0, 0, 0);
         }
+        if (!careful) {
+            float z = 0.f;                                   // NaN if a sum is not finite
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z = fmaf(oacc[ct][t][i], 0.f, z);
+            if (__builtin_expect(z != 0.f, 0)) words[1] = 1;
+            __syncthreads();
+            if (__builtin_expect(__builtin_amdgcn_readfirstlane(words[1]) != 0, 0)) {
+                careful = true;
+                goto again;
+            }
+        }
     }
 
     // ---- rows out
@@ -353,6 +370,11 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
         float l = l_run[t];
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
+        if (lo[t] >= hi[t]) {                                // a row without keys
+            l = 0.f;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) oacc[ct][t] = zero4;
+        }
         inv[t] = l == 0.f ? 0.f : 1.f / l;                   // (a NaN stays one)
         lse2[t] = l == 0.f ? -INFINITY : m_run[t] + log2f(l) + shift;
     }
@@ -403,7 +425,7 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
 
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(words[0]) == 0, 1)) return;
     constexpr int T1 = QT - 1;                               // (a wavefront of one tile: its second one has no keys)
-    dense_repair<__bf16, D, CAP, BIAS>(a, b, hk, m0, lane, part0, k_first, k_end, tile_lo, tile_hi, lo[0], QT == 2 ? lo[T1] : 0, hi[0],
+    dense_repair<__bf16, D, CAP, BIAS>(a, b, hk, m0, lane, part0, k_first, k_end, careful ? INT32_MAX : 0, k_end, lo[0], QT == 2 ? lo[T1] : 0, hi[0],
                                        QT == 2 ? hi[T1] : 0, lse2[0], lse2[T1]);
 }
 

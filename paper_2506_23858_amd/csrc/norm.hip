@@ -7,6 +7,7 @@
 // up in a fixed order by a second, small launch.
 #include "common.h"
 
+#include <cfloat>
 #include <cmath>
 
 namespace {
@@ -99,11 +100,18 @@ __device__ __forceinline__ void load_weight(const NormArgs& a, int lane, float (
 }
 struct RowAt { int b, h, s; };
 __device__ __forceinline__ RowAt row_at(long long r, const NormArgs& a) {      // rows in the order (b, s, h)
-    const long long bs = r / a.Hh;
     RowAt q;
-    q.h = (int)(r - bs * a.Hh);
-    q.b = (int)(bs / a.S);
-    q.s = (int)(bs - (long long)q.b * a.S);
+    if (a.rows < (1LL << 31)) {                              // (a 64-bit division is some hundred instructions)
+        const unsigned u = (unsigned)r, bs = a.Hh == 1 ? u : u / (unsigned)a.Hh;
+        q.h = (int)(u - bs * (unsigned)a.Hh);
+        q.b = bs < (unsigned)a.S ? 0 : (int)(bs / (unsigned)a.S);
+        q.s = (int)(bs - (unsigned)q.b * (unsigned)a.S);
+    } else {
+        const long long bs = r / a.Hh;
+        q.h = (int)(r - bs * a.Hh);
+        q.b = (int)(bs / a.S);
+        q.s = (int)(bs - (long long)q.b * a.S);
+    }
     return q;
 }
 template <class T>
@@ -172,7 +180,8 @@ __global__ __launch_bounds__(256) void rmsnorm_fwd_kernel(NormArgs a) {
                 }
             // (a NaN that the maximum passes over makes the whole row's scale one)
             top = reduce<L, true>(nan ? INFINITY : top, lds);
-            const float scale = top == INFINITY ? NAN : top / 448.f > 0.f ? top / 448.f : 1.f;
+            const bool some = top / 448.f > 0.f;
+            const float scale = top == INFINITY ? NAN : some ? top / 448.f : 1.f, up = top == INFINITY ? NAN : some ? fminf(448.f / top, FLT_MAX) : 1.f;
             if (lane == 0) a.y_scale[r] = scale;
             uint8_t* y = (uint8_t*)a.y.ptr + q.b * a.y.stride_b + q.s * a.y.stride_s + q.h * a.y.stride_h;
 #pragma unroll
@@ -180,8 +189,8 @@ __global__ __launch_bounds__(256) void rmsnorm_fwd_kernel(NormArgs a) {
                 const int d0 = (c * L + lane) * VEC;
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
-                    const float v = t[c][j] / scale;
-                    t[c][j] = v > 448.f ? 448.f : v < -448.f ? -448.f : v;      // the quotient's rounding can pass the largest value
+                    const float v = t[c][j] * up;
+                    t[c][j] = v > 448.f ? 448.f : v < -448.f ? -448.f : v;      // the roundings can pass the largest value
                 }
                 if (d0 < a.D) store_piece8<ALIGNED, VEC>(y, d0, a.D, t[c]);
             }
@@ -278,18 +287,21 @@ __global__ __launch_bounds__(256) void rmsnorm_bwd_kernel(NormArgs a) {
     }
 }
 
-// dweight[d] = sum of the workgroups' rows, in a fixed order: 16 channels x 16 interleaved shares of the rows per workgroup
-__global__ __launch_bounds__(256) void rmsnorm_dweight_kernel(const float* __restrict__ partial, float* __restrict__ dweight, int n, int D) {
-    __shared__ float sums[16][17];
+// dweight[d] = sum of the workgroups' rows, in a fixed order: 16 channels x 64 interleaved shares of the rows per workgroup
+__global__ __launch_bounds__(1024) void rmsnorm_dweight_kernel(const float* __restrict__ partial, float* __restrict__ dweight, int n, int D) {
+    __shared__ float sums[64][17];
     const int d = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
     float s = 0.f;
-    if (d < D)
-        for (int i = part; i < n; i += 16) s += partial[(long long)i * D + d];
+    if (d < D) {
+#pragma unroll 8
+        for (int i = part; i < n; i += 64) s += partial[(long long)i * D + d];
+    }
     sums[part][threadIdx.x % 16] = s;
     __syncthreads();
     if (part == 0 && d < D) {
         float t = 0.f;
-        for (int i = 0; i < 16; ++i) t += sums[i][threadIdx.x % 16];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) t += sums[i][threadIdx.x % 16];
         dweight[d] = t;
     }
 }
@@ -314,7 +326,9 @@ int64_t groups_grid(int64_t rows, int groups_per_wg, int64_t most) {
     return need < most ? need : most;
 }
 // Workgroups of the backward call, which is also the number of partial rows of dweight.
-constexpr int64_t BWD_WORKGROUPS = 1024;
+constexpr int64_t BWD_WORKGROUPS = 768;
+
+constexpr int64_t FWD_WORKGROUPS = 1280;
 
 bool norm_tensor_ok(const vmoba_tensor* t, int dtype) {
     const int es = dtype == VMOBA_F8E4M3 ? 1 : dtype_size(dtype);
@@ -398,7 +412,7 @@ extern "C" int vmoba_rmsnorm_fwd(int B, int Hh, int64_t S, int D, const vmoba_te
     const bool aligned = D % vec == 0 && aligned16(x, es, 16) && (out8 ? aligned16(y, 1, vec) : aligned16(y, es, 16)) &&
                          (!residual || (aligned16(residual, es, 16) && aligned16(total, es, 16)));
     const Shape shape = shape_for(D, vec);
-    const unsigned grid = (unsigned)groups_grid(a.rows, 256 / shape.L, 4096);
+    const unsigned grid = (unsigned)groups_grid(a.rows, 256 / shape.L, FWD_WORKGROUPS);
     hipStream_t st = (hipStream_t)stream;
 #define BY_ALIGNMENT(T, OUT8)                                        \
     do {                                                             \
@@ -451,7 +465,7 @@ extern "C" int vmoba_rmsnorm_bwd(int B, int Hh, int64_t S, int D, const vmoba_te
         VMOBA_CHECK_LAUNCH();
     }
     if (dweight) {
-        rmsnorm_dweight_kernel<<<dim3((unsigned)ceil_div64(D, 16)), dim3(256), 0, st>>>((const float*)workspace, dweight, a.rows > 0 ? (int)grid : 0, D);
+        rmsnorm_dweight_kernel<<<dim3((unsigned)ceil_div64(D, 16)), dim3(1024), 0, st>>>((const float*)workspace, dweight, a.rows > 0 ? (int)grid : 0, D);
         VMOBA_CHECK_LAUNCH();
     }
     return VMOBA_OK;

@@ -229,8 +229,8 @@ extern "C" int vmoba_rope(int B, int64_t S, int D, int n_tensors, const int32_t*
     const bool aligned = a.P % vec == 0 && (D - R) % vec == 0;
     const int64_t blocks = ceil_div64(a.tokens * (a.chunks + a.tail_chunks), 256);
     if (blocks > INT32_MAX) return VMOBA_ERR_UNSUPPORTED;
-    // Few tokens: the heads are dealt to more threads, down to one each, until there are two workgroups per compute unit.
-    const int64_t parts = blocks >= 512 ? 1 : ceil_div64(512, blocks);
+    // The heads are dealt to more threads, down to one each, until there are eight workgroups per compute unit.
+    const int64_t parts = blocks >= 2048 ? 1 : ceil_div64(2048, blocks);
     a.heads_per_part = (int)ceil_div64(a.total_heads, parts < a.total_heads ? parts : a.total_heads);
     const dim3 g((unsigned)blocks, (unsigned)ceil_div64(a.total_heads, a.heads_per_part));
     hipStream_t st = (hipStream_t)stream;
