@@ -473,12 +473,15 @@ class LayerPlan:
     where the caller has it, a query's id is its token index everywhere (P, mask, lists, LSE), and O,
     dO, dQ need no row map at all; dK and dV go back through key_rows = perm.
     With kv_in_place (implies q_in_place) nothing is rearranged in memory at all: the partition call only
-    builds the index arrays and every kernel finds key position k at row perm[k] of the caller's K and V."""
+    builds the index arrays and every kernel finds key position k at row perm[k] of the caller's K and V.
+    prepare: a QueryKeyPlan whose norms and rotary positions Q and K pass through first; backward() then returns the gradients of
+    what was given to forward()."""
 
     def __init__(self, B, Hh, D, grid, block=(0, 0, 0), chunk=0, tau=0.25, dtype=torch.bfloat16,
                  device="cuda", score_scale=None, softmax_scale=None, need_bwd=True, mode=GLOBAL_THRESHOLD, topk=0,
-                 fused_io=False, q_in_place=False, kv_in_place=False):
+                 fused_io=False, q_in_place=False, kv_in_place=False, prepare=None):
         T, H, W = grid
+        self.prepare = prepare
         self.kv_in_place = bool(kv_in_place)
         self.q_in_place = bool(q_in_place) or self.kv_in_place
         self.fused_io = bool(fused_io) or self.q_in_place
@@ -601,6 +604,8 @@ class LayerPlan:
                         [self.dQ, self.dK, self.dV], self.perm, None, None)
 
     def forward(self, Q, K, V):
+        if self.prepare is not None:
+            Q, K = self.prepare.forward(Q, K)
         self.partition(Q, K, V)
         self.select()
         self.attn_fwd()
@@ -611,8 +616,114 @@ class LayerPlan:
     def backward(self, dO):
         if self.fused_io:
             self.attn_bwd(dO)
-            return self.dQ, self.dK, self.dV
-        self.partition_dO(dO)
-        self.attn_bwd()
-        self.unpartition_grads()
+        else:
+            self.partition_dO(dO)
+            self.attn_bwd()
+            self.unpartition_grads()
+        if self.prepare is not None:
+            return *self.prepare.backward(self.dQ, self.dK), self.dV
+        return self.dQ, self.dK, self.dV
+
+
+class QueryKeyPlan:
+    """What queries and keys pass through between the projections and the attention: a root-mean-square norm with a weight each, and rotary
+    positions on the latent grid (or given ones).  All buffers are allocated once; the methods allocate nothing.
+    dims: channels rotated per axis, None: no rotation.  norm: None, "head" (over the D channels of every head, weights [D]) or "token" (over all
+    heads of a token, weights [heads * D]).  The weights wq, wk are the caller's; gradients of theirs are in dwq, dwk after backward()."""
+
+    def __init__(self, B, Hq, Hkv, S, D, dims=None, grid=None, layout=ROPE_HALF, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, train_len=0,
+                 norm="head", wq=None, wk=None, eps=1e-6, dtype=torch.bfloat16, device="cuda", need_bwd=True):
+        if norm not in (None, "head", "token"):
+            raise ValueError("norm is None, 'head' or 'token'")
+        self.B, self.S, self.D, self.heads, self.dims, self.grid, self.layout = B, S, D, (Hq, Hkv), dims, grid, layout
+        self.norm, self.weights, self.eps = norm, (wq, wk), eps
+        if dims is not None:
+            freqs, self.mscale = vmoba_rope_freqs(dims, base, scaling, factor, train_len)
+            self.freqs = freqs.to(device)
+        new = lambda: [torch.empty(B, S, h, D, dtype=dtype, device=device) for h in self.heads]      # noqa: E731
+        self.out, self.grads = new(), new() if need_bwd else None
+        if norm is not None:
+            sizes = [self._rows(h) for h in self.heads]
+            self.inv_rms = [torch.empty(B, S, n, device=device) for n, _ in sizes]
+            if need_bwd:
+                self.dwq, self.dwk = (torch.empty(d, device=device) for _, d in sizes)
+                n = max(vmoba_rmsnorm_workspace_bytes(B, n, S, d) for n, d in sizes)
+                self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+
+    def _rows(self, heads):
+        """Rows per token and channels per row of the norm."""
+        return (heads, self.D) if self.norm == "head" else (1, heads * self.D)
+
+    def _view(self, t, heads):
+        return t.view(self.B, self.S, *self._rows(heads))
+
+    def _rotate(self, src, dst, inverse, first, positions):
+        vmoba_rope(self.B, self.S, self.D, src, dst, self.freqs, self.dims, self.layout, inverse, self.mscale, self.grid, first, positions)
+
+    def forward(self, Q, K, first=0, positions=None):
+        """Q: [B, S, Hq, D], K: [B, S, Hkv, D]; first, positions: as in vmoba_rope.  Q and K are read again by backward()."""
+        self.inputs, self.at = (Q, K), (first, positions)
+        src = [Q, K]
+        if self.norm is not None:
+            for x, y, w, inv, h in zip(src, self.out, self.weights, self.inv_rms, self.heads):
+                n, d = self._rows(h)
+                vmoba_rmsnorm_fwd(self.B, n, self.S, d, self._view(x, h), None, w, self.eps, None, self._view(y, h), None, inv)
+            src = self.out
+        if self.dims is not None:
+            self._rotate(src, self.out, False, *self.at)
+            src = self.out
+        return src[0], src[1]
+
+    def backward(self, dQ, dK):
+        """Gradients of forward()'s inputs, from those of its outputs."""
+        src = [dQ, dK]
+        if self.dims is not None:
+            self._rotate(src, self.grads, True, *self.at)
+            src = self.grads
+        if self.norm is not None:
+            for x, dy, dx, w, inv, h, dw in zip(self.inputs, src, self.grads, self.weights, self.inv_rms, self.heads, (self.dwq, self.dwk)):
+                n, d = self._rows(h)
+                vmoba_rmsnorm_bwd(self.B, n, self.S, d, self._view(x, h), w, inv, self._view(dy, h), None, self._view(dx, h),
+                                  None if w is None else dw, self.workspace)
+            src = self.grads
+        return src[0], src[1]
+
+
+class DensePlan:
+    """Dense attention in the place of a sparse layer -- the layers and sampling steps that stay dense, packed clips, a prefix of text, a cache -- with all
+    buffers allocated once.  doc_off, prefix: int32 tensors on the device, read at every forward() (see vmoba_key_ranges).  prepare: as in LayerPlan."""
+
+    def __init__(self, B, Hq, Hkv, Sq, Sk, D, dtype=torch.bfloat16, device="cuda", softmax_scale=None, cap=0.0, slopes=None, doc_off=None, prefix=None,
+                 causal=False, need_bwd=True, prepare=None):
+        self.size, self.prepare = (B, Hq, Hkv, Sq, Sk, D), prepare
+        self.ranges = dict(doc_off=doc_off, prefix=prefix, causal=causal)
+        self.ranged = doc_off is not None or prefix is not None or causal
+        self.scores = dict(softmax_scale=1.0 / math.sqrt(D) if softmax_scale is None else softmax_scale, cap=cap, slopes=slopes)
+        code = VMOBA_BF16 if dtype == torch.bfloat16 else VMOBA_F32
+        n = max(vmoba_dense_workspace_bytes(op, *self.size, code) for op in ([OP_ATTN_FWD, OP_ATTN_BWD] if need_bwd else [OP_ATTN_FWD]))
+        if n == 0:
+            raise VmobaError("vmoba_dense_workspace_bytes", -2)
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        self.O = torch.empty(B, Sq, Hq, D, dtype=dtype, device=device)
+        self.LSE = torch.empty(B, Hq, Sq, device=device)
+        self.key_lo, self.key_hi = (torch.empty(B, Sq, dtype=torch.int32, device=device) for _ in range(2))
+        if need_bwd:
+            self.dQ, self.dK, self.dV = (torch.empty(B, s, h, D, dtype=dtype, device=device) for s, h in ((Sq, Hq), (Sk, Hkv), (Sk, Hkv)))
+
+    def forward(self, Q, K, V, q_pos=None):
+        """q_pos: int32 [B, Sq], positions of the queries among the keys; None: the last Sq ones."""
+        B, _, _, Sq, Sk, _ = self.size
+        if self.prepare is not None:
+            Q, K = self.prepare.forward(Q, K)
+        self.inputs, self.how = (Q, K, V), dict(self.scores, q_pos=q_pos, q_first=Sk - Sq)
+        if self.ranged:
+            vmoba_key_ranges(B, Sq, Sk, self.key_lo, self.key_hi, q_pos=q_pos, q_first=Sk - Sq, **self.ranges)
+            self.how.update(key_lo=self.key_lo, key_hi=self.key_hi)
+        vmoba_dense_fwd(*self.size, Q, K, V, self.O, self.LSE, self.workspace, **self.how)
+        return self.O
+
+    def backward(self, dO):
+        vmoba_dense_bwd(*self.size, *self.inputs, self.O, self.LSE, dO, self.dQ, self.dK, self.dV, self.workspace, **self.how)
+        if self.prepare is not None:
+            return *self.prepare.backward(self.dQ, self.dK), self.dV
         return self.dQ, self.dK, self.dV

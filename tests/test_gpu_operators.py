@@ -171,10 +171,15 @@ def test_norm_rows_of_zeros_infinities_and_nan():
         assert float(y8[0, r].float().abs().max()) == 448.0
 
 
-def test_norm_without_rows():
-    x = torch.empty(1, 0, 1, 64, dtype=BF16, device="cuda")
-    y, inv, dw = torch.empty_like(x), torch.empty(1, 0, 1, device="cuda"), torch.full((64,), 3.0, device="cuda")
+def test_calls_without_rows():
+    """The binding hands out no address for an empty tensor; the library takes any and launches nothing but the clearing of dweight."""
     assert vb.vmoba_rmsnorm_workspace_bytes(1, 1, 0, 64) == 0
+    some, dw = torch.empty(64, dtype=BF16, device="cuda"), torch.full((64,), 3.0, device="cuda")
+    d = vb._desc(some.view(1, 1, 1, 64))
+    L, st = vb.lib(), torch.cuda.current_stream().cuda_stream
+    assert L.vmoba_rmsnorm_fwd(1, 1, 0, 64, d, None, None, 0, 1e-6, None, d, None, None, st) == 0
+    assert L.vmoba_rmsnorm_bwd(1, 1, 0, 64, d, None, 0, dw.data_ptr(), d, None, d, dw.data_ptr(), None, 0, st) == 0
+    assert bool((dw == 0).all())
 
 
 # ---------------------------------------------------------------------------------------------------------------- dense attention
@@ -387,3 +392,101 @@ def test_dense_streams_graphs_and_repeats():
         torch.cuda.synchronize()
         assert all(torch.equal(first[k], out[k]) for k in first)
         assert torch.equal(run(Q, K, V, dO)["dK"], first["dK"])
+
+
+# ---------------------------------------------------------------------------------------------------------------- together
+def layer_reference(Q, K, V, wq, wk, dims, grid, norm, dO, cap):
+    """Norm, rotation, dense attention in 64 bits, and their gradients by automatic differentiation."""
+    leaves = [t.double().detach().requires_grad_() for t in (Q, K, V, wq, wk)]
+    q, k, v, a, b = leaves
+
+    def prepared(x, w):
+        y = x if norm == "head" else x.flatten(2)
+        y = (y * (y.square().mean(-1, keepdim=True) + 1e-6).rsqrt() * w).view(x.shape)
+        freqs = torch.cat([1e4 ** (-torch.arange(0, d, 2, dtype=torch.float64, device="cuda") / d) for d in dims])
+        axis = torch.repeat_interleave(torch.arange(len(dims), device="cuda"), torch.tensor([d // 2 for d in dims], device="cuda"))
+        at = torch.stack(torch.meshgrid(*[torch.arange(n, device="cuda") for n in grid], indexing="ij"), -1).reshape(-1, 3).double()
+        z = torch.view_as_complex(y[..., :sum(dims)].reshape(*y.shape[:-1], -1, 2)) * torch.polar(torch.ones_like(at[:, axis]), at[:, axis] * freqs)[:, None]
+        return torch.cat([torch.view_as_real(z).flatten(-2), y[..., sum(dims):]], -1)
+
+    G = Q.shape[2] // K.shape[2]
+    s = torch.einsum("bqhd,bkhd->bhqk", prepared(q, a), prepared(k, b).repeat_interleave(G, 2)) / math.sqrt(Q.shape[3])
+    s = cap * torch.tanh(s / cap) if cap else s
+    o = torch.einsum("bhqk,bkhd->bqhd", s.softmax(-1), v.repeat_interleave(G, 2))
+    (o * dO.double()).sum().backward()
+    return o.detach(), [t.grad for t in leaves]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("norm", ["head", "token"])
+@pytest.mark.parametrize("kind", ["dense", "sparse"])
+def test_a_layer_with_norms_and_positions(kind, norm, dtype):
+    """QueryKeyPlan in front of a dense plan, and of a sparse plan that keeps every pair (tau = 1), forward and backward."""
+    grid, dims, B, Hq, D = (3, 5, 7), [24, 20, 20], 1, 4, 64
+    Hkv = 2 if kind == "dense" else 4
+    S, cap = 105, 20.0 if kind == "dense" else 0.0
+    Q, K, V = ou.normal(1, (B, S, Hq + 2 * Hkv, D), dtype).split([Hq, Hkv, Hkv], 2)
+    dO = ou.normal(2, (B, S, Hq, D), dtype)
+    wq, wk = (1 + 0.1 * ou.normal(3 + i, (D if norm == "head" else h * D,), F32) for i, h in enumerate((Hq, Hkv)))
+    prepare = vb.QueryKeyPlan(B, Hq, Hkv, S, D, dims, grid, vb.ROPE_INTERLEAVED, norm=norm, wq=wq, wk=wk, dtype=dtype)
+    if kind == "dense":
+        plan = vb.DensePlan(B, Hq, Hkv, S, S, D, dtype, cap=cap, prepare=prepare)
+    else:
+        plan = vb.LayerPlan(B, Hq, D, grid, (3, 5, 3), tau=1.0, dtype=dtype, q_in_place=True, prepare=prepare)
+    O = plan.forward(Q, K, V).clone()
+    grads = [*(t.clone() for t in plan.backward(dO)), prepare.dwq, prepare.dwk]
+    ref, want = layer_reference(Q, K, V, wq, wk, dims, grid, norm, dO, cap)
+    # The outputs of norm and rotation are rounded to the type (twice), weights, dz, O and the gradients once more each: six roundings, whose
+    # relative errors add up in the 2-norm at worst
+    bound = 6 * ou.HALF[dtype] if dtype == BF16 else 2e-5
+    for name, got, value in zip(("O", "dQ", "dK", "dV", "dwq", "dwk"), [O] + grads, [ref] + want):
+        rel = float((got.double() - value).norm() / value.norm())
+        print(f"   {name}: relative error {rel:.2e} of {bound:.2e}", flush=True)
+        assert rel <= bound, name
+
+
+def test_a_token_against_a_cache_with_positions():
+    """A step of serving: the new token's query and key are normalised and turned at its own position, the key joins the cache, and the query
+    reads the cache as far as its sequence goes -- the same as the last row of the whole sequence."""
+    B, Hq, Hkv, S, D = 2, 8, 2, 150, 64
+    Q, K, V = ou.normal(1, (B, S, Hq + 2 * Hkv, D), BF16).split([Hq, Hkv, Hkv], 2)
+    w = 1 + 0.1 * ou.normal(2, (D,), F32)
+    args = dict(dims=[32], scaling=vb.ROPE_YARN, factor=4.0, train_len=64, wq=w, wk=w, need_bwd=False)
+    whole = vb.QueryKeyPlan(B, Hq, Hkv, S, D, **args)
+    q, k = whole.forward(Q, K)
+    full = vb.DensePlan(B, Hq, Hkv, S, S, D, causal=True, need_bwd=False).forward(q, k, V)
+    step = vb.QueryKeyPlan(B, Hq, Hkv, 1, D, **args)
+    lens = [S, 83]
+    at = int32([[n - 1] for n in lens])
+    cache_k, cache_v = (torch.full((B, 256, Hkv, D), math.nan, dtype=BF16, device="cuda") for _ in range(2))
+    for b, n in enumerate(lens):
+        cache_k[b, :n], cache_v[b, :n] = k[b, :n], V[b, :n]
+    qt, kt = step.forward(torch.stack([Q[b, n - 1:n] for b, n in enumerate(lens)]), torch.stack([K[b, n - 1:n] for b, n in enumerate(lens)]),
+                          positions=at[:, :, None].contiguous())
+    for b, n in enumerate(lens):
+        assert torch.equal(kt[b, 0], k[b, n - 1])
+        assert torch.equal(qt[b, 0], q[b, n - 1])
+    plan = vb.DensePlan(B, Hq, Hkv, 1, 256, D, doc_off=int32([[0, n] for n in lens]), causal=True, need_bwd=False)
+    got = plan.forward(qt, cache_k, cache_v, q_pos=at)
+    for b, n in enumerate(lens):
+        ref = ou.attention(q[b:b + 1, n - 1:n], k[b:b + 1, :n], V[b:b + 1, :n], int32([[0]]), int32([[n]]), None, 0.125)["O"]
+        ou.within("token", got[b:b + 1], *ref)
+        ou.within("row of the whole", full[b:b + 1, n - 1:n], *ref)
+
+
+def test_rows_behind_the_last_sequence_stay_as_they_are():
+    """Calls on a part of a larger buffer touch nothing outside it."""
+    B, S, H, D, n = 1, 96, 2, 64, 61
+    big = {k: torch.full((B, S, H, D), 7.0, dtype=BF16, device="cuda") for k in ("O", "dQ", "dK", "dV", "y", "r")}
+    Q, K, V, dO = (ou.normal(i, (B, S, H, D), BF16) for i in range(4))
+    part = {k: v[:, :n] for k, v in big.items()}
+    lse = torch.empty(B, H, n, device="cuda")
+    ws = torch.empty(max(vb.vmoba_dense_workspace_bytes(op, B, H, H, n, n, D, vb.VMOBA_BF16) for op in (2, 3)), dtype=torch.uint8, device="cuda")
+    vb.vmoba_dense_fwd(B, H, H, n, n, D, Q[:, :n], K[:, :n], V[:, :n], part["O"], lse, ws, 0.125)
+    vb.vmoba_dense_bwd(B, H, H, n, n, D, Q[:, :n], K[:, :n], V[:, :n], part["O"], lse, dO[:, :n], part["dQ"], part["dK"], part["dV"], ws, 0.125)
+    vb.vmoba_rmsnorm_fwd(B, H, n, D, Q[:, :n], None, None, 1e-6, None, part["y"], None, None)
+    freqs, _ = vb.vmoba_rope_freqs([64])
+    vb.vmoba_rope(B, n, D, [Q[:, :n]], [part["r"]], freqs.cuda(), [64])
+    for k, v in big.items():
+        assert bool((v[:, n:] == 7.0).all()), k
+        assert not bool((v[:, :n] == 7.0).all()), k
