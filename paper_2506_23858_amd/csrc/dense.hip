@@ -85,19 +85,20 @@ __global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
     if (part == 0) a.LSE[((long long)b * a.Hq + h) * a.Sq + q] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * DENSE_LN2;
 }
 
-// Joins the splits of a backward call's dK and dV: sums in the order of the splits.
-template <class T, int D>
+// Joins the splits of a backward call's dQ (ROWS) or dK and dV: sums in the order of the splits.
+template <class T, int D, bool ROWS>
 __global__ __launch_bounds__(256) void dense_sum_kernel(DenseArgs a) {
     constexpr int LPR = D / 4;
-    const long long n = (long long)a.B * a.Hkv * a.Sk, i = ((long long)blockIdx.x * 256 + threadIdx.x) / LPR;
+    const long long n = (long long)a.B * a.Hkv * (ROWS ? a.M : a.Sk), all = ROWS ? n : 2 * n, i = ((long long)blockIdx.x * 256 + threadIdx.x) / LPR;
     const int part = threadIdx.x % LPR;
-    if (i >= 2 * n) return;
-    const long long row = i < n ? i : i - n;
+    if (i >= all) return;
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) acc += *reinterpret_cast<const f32x4_t*>(a.part_o + (2 * s * n + i) * D + part * 4);
-    const int bh = (int)(row / a.Sk), key = (int)(row - (long long)bh * a.Sk), b = bh / a.Hkv, hk = bh - b * a.Hkv;
-    char* dst = const_cast<char*>(row_ptr(i < n ? a.dK : a.dV, b, key, hk, sizeof(T)));
+    for (int s = 0; s < a.splits; ++s) acc += *reinterpret_cast<const f32x4_t*>(a.part_o + (s * all + i) * D + part * 4);
+    const int per = ROWS ? a.M : a.Sk;
+    const long long row = i < n ? i : i - n;
+    const int bh = (int)(row / per), r = (int)(row - (long long)bh * per), b = bh / a.Hkv, hk = bh - b * a.Hkv, q = ROWS ? query_of(a, r) : r;
+    char* dst = const_cast<char*>(row_ptr(ROWS ? a.dQ : i < n ? a.dK : a.dV, b, q, ROWS ? hk * a.G + (r - q * a.G) : hk, sizeof(T)));
     if constexpr (sizeof(T) == 2) {
         const u32x2_t v = {pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
         *reinterpret_cast<u32x2_t*>(dst + part * 8) = v;
@@ -243,28 +244,33 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     }
 }
 
-// Key splits of a forward call: as many workgroups as run at a time (two per compute unit), at least 128 keys each.  One query
-// of 16 heads on 4 key heads, 8 sequences of 32 760 keys: 32 tiles on 512 places.
-int splits_for(int64_t tiles, int64_t Sk) {
-    const int64_t places = 512, by_places = places / std::max<int64_t>(tiles, 1), by_keys = ceil_div64(Sk, 128);
+// Splits of a row tile's keys.  Without key ranges: as many pieces as run at a time (two per compute unit), at least 128 keys each; one query
+// of 16 heads on 4 key heads, 8 sequences of 32 760 keys: 32 tiles on 512 places.  With ranges tiles cost different amounts, and the longest of a few that all
+// run at once decides: for float32 four times as many pieces, at least 256 keys each, unless there are so many tiles that their order evens them out (2 x 2001 tokens, 16 heads on
+// 4, 64 channels, causal, forward and backward: 1450 -> 900 us).  bfloat16 keeps to one round: its groups of keys take a quarter of the time, and pieces' ends
+// cost as much (1637 tokens x 12 heads, causal: 49 us, 74 with four times the pieces).
+int splits_for(int64_t tiles, int64_t Sk, bool uneven) {
+    const int64_t pieces = uneven && tiles <= 640 ? 2048 : 512, by_places = pieces / std::max<int64_t>(tiles, 1), by_keys = ceil_div64(Sk, uneven ? 256 : 128);
     return (int)std::max<int64_t>(1, std::min(by_places, by_keys));
 }
-
 // Row splits of the dK/dV kernel, the same with at least 256 rows each.
-int row_splits_for(int64_t tiles, int64_t M) {
-    return (int)std::max<int64_t>(1, std::min(512 / std::max<int64_t>(tiles, 1), M / 256));
+int row_splits_for(int64_t tiles, int64_t M, bool uneven) {
+    const int64_t pieces = uneven && tiles <= 640 ? 2048 : 512;
+    return (int)std::max<int64_t>(1, std::min(pieces / std::max<int64_t>(tiles, 1), M / 256));
 }
 // More pieces of work than run at a time: their order matters.
 bool order_matters(int64_t pieces) { return pieces > 512; }
 
 struct Sizes {
-    int G, splits, row_splits, rows_per_tile;
+    int G, rows_per_tile;
+    int splits, dq_splits, row_splits;         // forward and dQ: of a row tile's keys; dK/dV: of a key tile's rows
     int64_t M, q_tiles, k_tiles, chunks;       // tiles and chunks of all batch elements and key heads
     size_t part_lse, part_o, order, fwd;       // forward workspace: offsets, bytes
     size_t info, bounds, order_b, part_b, bwd; // backward
 };
 // false: not a supported geometry
-bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, Sizes& z) {
+// uneven: float32 with key ranges
+bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool uneven, Sizes& z) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv || (D != 64 && D != 128)) return false;
     z.G = Hq / Hkv;
     if (Sq >= (1 << 24) || Sk >= (1 << 24) || Sq * z.G >= (1 << 24)) return false;
@@ -275,8 +281,10 @@ bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, Sizes& z) {
     z.k_tiles = BH * ceil_div64(Sk, DENSE_TILE_ROWS);
     z.chunks = BH * ceil_div64(z.M, 32);
     if (z.q_tiles > (1 << 22) || z.k_tiles > (1 << 22) || z.chunks > (1 << 24)) return false;
-    z.splits = splits_for(z.q_tiles, Sk);
-    z.row_splits = row_splits_for(z.k_tiles, z.M);
+    const bool few = z.M <= DENSE_FEW_ROWS;    // (single queries: bytes are what counts, and a piece's share of them is even enough)
+    z.splits = splits_for(z.q_tiles, Sk, uneven && !few);
+    z.dq_splits = splits_for(BH * ceil_div64(z.M, DENSE_TILE_ROWS), Sk, uneven);
+    z.row_splits = row_splits_for(z.k_tiles, z.M, uneven);
     size_t off = 0;
     auto take = [&](int64_t bytes) {
         const size_t at = off;
@@ -285,13 +293,13 @@ bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, Sizes& z) {
     };
     z.part_lse = take(z.splits > 1 ? z.splits * BH * z.M * 4 : 0);
     z.part_o = take(z.splits > 1 ? z.splits * BH * z.M * D * 4 : 0);
-    z.order = take(order_matters(z.q_tiles) ? 2 * (z.q_tiles / Hkv) * 4 : 0);
+    z.order = take(order_matters(z.q_tiles * z.splits) ? 2 * (z.q_tiles / Hkv) * 4 : 0);
     z.fwd = std::max<size_t>(off, 256);
     off = 0;
     z.info = take(z.chunks * (int64_t)sizeof(RowInfo));
     z.bounds = take(z.chunks * (int64_t)sizeof(int4));
     z.order_b = take(2 * (B * ceil_div64(z.M, DENSE_TILE_ROWS) + z.k_tiles / Hkv) * 4);
-    z.part_b = take(z.row_splits > 1 ? 2 * z.row_splits * BH * Sk * D * 4 : 0);
+    z.part_b = take(std::max<int64_t>(z.row_splits > 1 ? 2 * z.row_splits * BH * Sk : 0, z.dq_splits > 1 ? z.dq_splits * BH * z.M : 0) * D * 4);
     z.bwd = off;
     return true;
 }
@@ -310,7 +318,7 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
     if ((how->key_lo != nullptr) != (how->key_hi != nullptr)) return VMOBA_ERR_INVALID_ARG;
     if (how->q_first < INT32_MIN || how->q_first + Sq > INT32_MAX) return VMOBA_ERR_INVALID_ARG;
     if (K->dtype != Q->dtype || V->dtype != Q->dtype || O->dtype != Q->dtype) return VMOBA_ERR_UNSUPPORTED;
-    if (!sizes_of(B, Hq, Hkv, Sq, Sk, D, z)) return VMOBA_ERR_UNSUPPORTED;
+    if (!sizes_of(B, Hq, Hkv, Sq, Sk, D, how->key_lo != nullptr && Q->dtype == VMOBA_F32, z)) return VMOBA_ERR_UNSUPPORTED;
     if (!reach_ok(K, Sk) || !reach_ok(V, Sk)) return VMOBA_ERR_UNSUPPORTED;
     a.Q = make_view(Q);
     a.K = make_view(K);
@@ -346,9 +354,9 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
 }  // namespace
 
 extern "C" size_t vmoba_dense_workspace_bytes(int op, int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, int dtype) {
-    Sizes z;
-    if ((dtype != VMOBA_F32 && dtype != VMOBA_BF16) || !sizes_of(B, Hq, Hkv, Sq, Sk, D, z)) return 0;
-    return op == VMOBA_OP_ATTN_FWD ? z.fwd : op == VMOBA_OP_ATTN_BWD ? z.bwd : 0;
+    Sizes y, z;      // whether there are key ranges is not known here
+    if ((dtype != VMOBA_F32 && dtype != VMOBA_BF16) || !sizes_of(B, Hq, Hkv, Sq, Sk, D, false, y) || !sizes_of(B, Hq, Hkv, Sq, Sk, D, dtype == VMOBA_F32, z)) return 0;
+    return op == VMOBA_OP_ATTN_FWD ? std::max(y.fwd, z.fwd) : op == VMOBA_OP_ATTN_BWD ? std::max(y.bwd, z.bwd) : 0;
 }
 
 extern "C" int vmoba_key_ranges(int B, int64_t Sq, int64_t Sk, const int32_t* doc_off, int64_t doc_stride_b, int32_t n_docs, const int32_t* prefix,
@@ -370,14 +378,14 @@ extern "C" int vmoba_dense_fwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
     DenseArgs a{};
     if (const int rc = check(B, Hq, Hkv, Sq, Sk, D, Q, K, V, how, O, LSE, z, a)) return rc;
     if (!workspace || (uintptr_t)workspace & 255) return VMOBA_ERR_INVALID_ARG;
-    if (workspace_bytes < z.fwd) return VMOBA_ERR_WORKSPACE;
+    if (workspace_bytes < vmoba_dense_workspace_bytes(VMOBA_OP_ATTN_FWD, B, Hq, Hkv, Sq, Sk, D, Q->dtype)) return VMOBA_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const bool bf16 = Q->dtype == VMOBA_BF16, cap = how->cap > 0.f;
     a.splits = z.splits;
     char* const ws = (char*)workspace;
     a.part_lse = (float*)(ws + z.part_lse);
     a.part_o = (float*)(ws + z.part_o);
-    if (a.key_lo && order_matters(z.q_tiles)) {
+    if (a.key_lo && order_matters(z.q_tiles * z.splits)) {
         int* order = (int*)(ws + z.order);
         dense_order_kernel<<<dim3(1), dim3(1024), 0, st>>>(a, OrderArgs{order, order + z.q_tiles / Hkv, nullptr, nullptr, z.rows_per_tile});
         VMOBA_CHECK_LAUNCH();
@@ -406,7 +414,7 @@ extern "C" int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
     if (const int rc = check(B, Hq, Hkv, Sq, Sk, D, Q, K, V, how, O, LSE, z, a)) return rc;
     if (!tensor_ok(dO) || !tensor_ok(dQ) || !tensor_ok(dK) || !tensor_ok(dV) || !workspace || (uintptr_t)workspace & 255) return VMOBA_ERR_INVALID_ARG;
     if (dO->dtype != Q->dtype || dQ->dtype != Q->dtype || dK->dtype != Q->dtype || dV->dtype != Q->dtype) return VMOBA_ERR_UNSUPPORTED;
-    if (workspace_bytes < z.bwd) return VMOBA_ERR_WORKSPACE;
+    if (workspace_bytes < vmoba_dense_workspace_bytes(VMOBA_OP_ATTN_BWD, B, Hq, Hkv, Sq, Sk, D, Q->dtype)) return VMOBA_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const bool bf16 = Q->dtype == VMOBA_BF16, cap = how->cap > 0.f;
     // packed rows of Q and dO by 32-bit offsets
@@ -422,7 +430,6 @@ extern "C" int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
     a.row_info = ws + z.info;
     a.row_bounds = (int4*)(ws + z.bounds);
     a.part_o = (float*)(ws + z.part_b);
-    a.splits = z.row_splits;
     const dim3 grid((unsigned)z.chunks);
     if (bf16 && D == 128) dense_rows_kernel<__bf16, 128><<<grid, dim3(256), 0, st>>>(a);
     else if (bf16) dense_rows_kernel<__bf16, 64><<<grid, dim3(256), 0, st>>>(a);
@@ -430,23 +437,32 @@ extern "C" int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
     else dense_rows_kernel<float, 64><<<grid, dim3(256), 0, st>>>(a);
     VMOBA_CHECK_LAUNCH();
     const int64_t nq = B * ceil_div64(z.M, DENSE_TILE_ROWS), nk = z.k_tiles / Hkv;
-    if (a.key_lo && order_matters(std::max(nq, nk) * Hkv)) {
+    if (a.key_lo && order_matters(std::max(nq * z.dq_splits, nk * z.row_splits) * Hkv)) {
         int* order = (int*)(ws + z.order_b);
         dense_order_kernel<<<dim3(2), dim3(1024), 0, st>>>(a, OrderArgs{order, order + nq, order + 2 * nq, order + 2 * nq + nk, DENSE_TILE_ROWS});
         VMOBA_CHECK_LAUNCH();
         a.order_q = order;
         a.order_k = order + 2 * nq;
     }
-    if (bf16) launch_dense_bwd_bf16(D, cap, st, a);
-    else launch_dense_bwd_f32(D, cap, st, a);
+    a.splits = z.dq_splits;
+    if (bf16) launch_dense_dq_bf16(D, cap, st, a);
+    else launch_dense_dq_f32(D, cap, st, a);
     VMOBA_CHECK_LAUNCH();
-    if (a.splits > 1) {
-        const dim3 sums((unsigned)ceil_div64(2 * (int64_t)B * Hkv * Sk * (D / 4), 256));
-        if (bf16 && D == 128) dense_sum_kernel<__bf16, 128><<<sums, dim3(256), 0, st>>>(a);
-        else if (bf16) dense_sum_kernel<__bf16, 64><<<sums, dim3(256), 0, st>>>(a);
-        else if (D == 128) dense_sum_kernel<float, 128><<<sums, dim3(256), 0, st>>>(a);
-        else dense_sum_kernel<float, 64><<<sums, dim3(256), 0, st>>>(a);
-        VMOBA_CHECK_LAUNCH();
-    }
+#define SUM(ROWS, COUNT)                                                                                             \
+    do {                                                                                                             \
+        const dim3 sums((unsigned)ceil_div64((COUNT) * (D / 4), 256));                                               \
+        if (bf16 && D == 128) dense_sum_kernel<__bf16, 128, ROWS><<<sums, dim3(256), 0, st>>>(a);                    \
+        else if (bf16) dense_sum_kernel<__bf16, 64, ROWS><<<sums, dim3(256), 0, st>>>(a);                            \
+        else if (D == 128) dense_sum_kernel<float, 128, ROWS><<<sums, dim3(256), 0, st>>>(a);                        \
+        else dense_sum_kernel<float, 64, ROWS><<<sums, dim3(256), 0, st>>>(a);                                       \
+        VMOBA_CHECK_LAUNCH();                                                                                        \
+    } while (0)
+    if (a.splits > 1) SUM(true, (int64_t)B * Hkv * z.M);
+    a.splits = z.row_splits;
+    if (bf16) launch_dense_dkv_bf16(D, cap, st, a);
+    else launch_dense_dkv_f32(D, cap, st, a);
+    VMOBA_CHECK_LAUNCH();
+    if (a.splits > 1) SUM(false, 2 * (int64_t)B * Hkv * Sk);
+#undef SUM
     return VMOBA_OK;
 }

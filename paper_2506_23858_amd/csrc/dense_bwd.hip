@@ -38,9 +38,9 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     __shared__ __align__(1024) char smem[2 * BUF + 64];
 
     const int tiles = (a.M + 127) / 128;
-    const DensePiece piece = dense_piece(a.B * tiles, a.Hkv);
+    const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
     if (piece.rank < 0) return;
-    const DenseTask task = dense_task(piece.rank, 1, tiles, a.order_q);
+    const DenseTask task = dense_task(piece.rank, a.splits, tiles, a.order_q);
     const int tile = task.tile, b = task.b, hk = piece.head, bh = b * a.Hkv + hk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
@@ -108,6 +108,8 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     if (tid == 0) words[0] = 0;                 // from here on: whether a sum is not finite
     int k_first = __builtin_amdgcn_readfirstlane(any_lo), k_end = __builtin_amdgcn_readfirstlane(any_hi);
     if (k_first >= k_end) k_first = k_end = 0;
+    split_keys<KC>(task.split, a.splits, k_first, k_end);
+    all_hi = min(all_hi, k_end);
     const int n_chunks = (k_end - k_first + KC - 1) / KC;
 
     const char *kbase = row_ptr(a.K, b, 0, hk, 2), *vbase = row_ptr(a.V, b, 0, hk, 2);
@@ -160,7 +162,7 @@ again:
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
             const int kb = kc + mt * 32;
-            if (kb + 32 > wave_lo && kb < wave_hi) {      // (keys that one of the wavefront's rows reads)
+            if (kb + 32 > wave_lo && kb < min(wave_hi, k_end)) {      // (keys that one of the wavefront's rows reads)
                 const bool masked = careful || kb < all_lo || kb + 32 > all_hi;
                 f32x4_t s[2][2], dp[2][2];            // [16 keys][16 rows]: value i is key 16 * kt + 4 * g + i
                 bf16x8_t ds[2];
@@ -191,7 +193,7 @@ again:
                         const int half = n == NP ? 1 : 0;
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
-                            const int first_key = lo[t] - kb - 4 * g - 16 * half, end = hi[t] - kb - 4 * g - 16 * half;
+                            const int first_key = lo[t] - kb - 4 * g - 16 * half, end = min(hi[t], k_end) - kb - 4 * g - 16 * half;
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
                                 if (i < first_key || i >= end) s[half][t][i] = -INFINITY;      // (with the cap: r = 1, so f = 0)
@@ -244,6 +246,18 @@ again:
             careful = true;
             goto again;
         }
+    }
+    if (a.splits > 1) {                         // this split's sums, added up by dense_sum_kernel
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int m = m0 + 16 * t + l16;
+            if (m < a.M) {
+                float* dst = a.part_o + (((long long)task.split * a.B * a.Hkv + bh) * a.M + m) * D + 4 * g;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<f32x4_t*>(dst + 16 * ct) = acc[ct][t] * a.scale;
+            }
+        }
+        return;
     }
     char* mine = smem + wave * 32 * OPITCH;
 #pragma unroll
@@ -536,21 +550,25 @@ again:
     }
 }
 
-template <int D>
-void launch_bwd(bool cap, hipStream_t st, const DenseArgs& a) {
-    const dim3 gq(dense_grid((int64_t)a.B * ceil_div64(a.M, 128), a.Hkv)), gk(dense_grid((int64_t)a.B * ceil_div64(a.Sk, 128) * a.splits, a.Hkv)), block(256);
-#define BOTH(CAP, BIAS)                                     \
-    do {                                                    \
-        dense_dq_kernel<D, CAP, BIAS><<<gq, block, 0, st>>>(a);   \
-        dense_dkv_kernel<D, CAP, BIAS><<<gk, block, 0, st>>>(a);  \
+#define BY_SCORES(KERNEL)                                                              \
+    do {                                                                               \
+        if (cap && a.slopes) KERNEL<D, true, true><<<grid, block, 0, st>>>(a);         \
+        else if (cap) KERNEL<D, true, false><<<grid, block, 0, st>>>(a);               \
+        else if (a.slopes) KERNEL<D, false, true><<<grid, block, 0, st>>>(a);          \
+        else KERNEL<D, false, false><<<grid, block, 0, st>>>(a);                       \
     } while (0)
-    if (cap && a.slopes) BOTH(true, true);
-    else if (cap) BOTH(true, false);
-    else if (a.slopes) BOTH(false, true);
-    else BOTH(false, false);
-#undef BOTH
+template <int D>
+void launch_dq(bool cap, hipStream_t st, const DenseArgs& a) {
+    const dim3 grid(dense_grid((int64_t)a.B * ceil_div64(a.M, 128) * a.splits, a.Hkv)), block(256);
+    BY_SCORES(dense_dq_kernel);
+}
+template <int D>
+void launch_dkv(bool cap, hipStream_t st, const DenseArgs& a) {
+    const dim3 grid(dense_grid((int64_t)a.B * ceil_div64(a.Sk, 128) * a.splits, a.Hkv)), block(256);
+    BY_SCORES(dense_dkv_kernel);
 }
 
 }  // namespace
 
-void launch_dense_bwd_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a) { D == 128 ? launch_bwd<128>(cap, st, a) : launch_bwd<64>(cap, st, a); }
+void launch_dense_dq_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a) { D == 128 ? launch_dq<128>(cap, st, a) : launch_dq<64>(cap, st, a); }
+void launch_dense_dkv_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a) { D == 128 ? launch_dkv<128>(cap, st, a) : launch_dkv<64>(cap, st, a); }

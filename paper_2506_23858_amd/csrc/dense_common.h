@@ -19,12 +19,13 @@ struct DenseArgs {
     const int *key_lo, *key_hi, *q_pos;
     long long q_first;
     float* LSE;
-    float *part_o, *part_lse;      // forward, more than one split: [splits][B * Hkv][M][D] and [splits][B * Hkv][M] (base 2)
+    float *part_o, *part_lse;      // more than one split: forward [splits][B * Hkv][M][D] and [splits][B * Hkv][M] (base 2); dQ [splits][B * Hkv][M][D];
+                                   // dK and dV [splits][2][B * Hkv][Sk][D]
     const int *order_q, *order_k;  // places by falling cost: [B * row tiles] and, backward, [B * key tiles]; null: as they come
     char* row_info;                // backward: ROW_INFO bytes per 32 rows, see RowInfo
     int4* row_bounds;              // backward: {lowest lo, highest hi, highest lo, lowest hi} of every 32 rows with keys
     int B, Hq, Hkv, G, Sq, Sk, M;
-    int splits;                    // of a tile's keys (forward), of a key tile's rows (dK/dV)
+    int splits;                    // of a row tile's keys (forward, dQ), of a key tile's rows (dK/dV)
     float scale, scale_log2;       // softmax_scale; max(|softmax_scale| log2 e, FLT_MIN)
     float cap2, cap_in, cap_arg;   // cap log2(e); 2 scale_log2 / cap; |softmax_scale| / cap
     unsigned G_magic;              // see query_of; 0: divide
@@ -220,10 +221,21 @@ __device__ __forceinline__ DenseTask dense_task(int rank, int splits, int tiles,
     return {b, bt - b * tiles, rank - place * splits};
 }
 
+// A split's share of keys first .. end - 1, in whole steps of STEP keys.
+template <int STEP>
+__device__ __forceinline__ void split_keys(int split, int splits, int& first, int& end) {
+    if (splits == 1) return;
+    const int steps = (end - first + STEP - 1) / STEP, per = (steps + splits - 1) / splits, s0 = min(split * per, steps), s1 = min(s0 + per, steps);
+    end = min(end, first + s1 * STEP);
+    first += s0 * STEP;
+}
+
 // Most rows of a tile that one wavefront takes alone, and the rows of the tile of four.
 constexpr int DENSE_FEW_ROWS = 32, DENSE_TILE_ROWS = 128;
 
 void launch_dense_fwd_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a);
 void launch_dense_fwd_f32(int D, bool cap, hipStream_t st, const DenseArgs& a);
-void launch_dense_bwd_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a);
-void launch_dense_bwd_f32(int D, bool cap, hipStream_t st, const DenseArgs& a);
+void launch_dense_dq_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a);
+void launch_dense_dq_f32(int D, bool cap, hipStream_t st, const DenseArgs& a);
+void launch_dense_dkv_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a);
+void launch_dense_dkv_f32(int D, bool cap, hipStream_t st, const DenseArgs& a);

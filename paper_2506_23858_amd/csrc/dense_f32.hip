@@ -150,12 +150,7 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
     const int pos = BIAS ? dense_position(a, b, q) : 0;
     const Keys keys = tile_keys<NW>(lo, hi, wave, lane, words);
     int k_first = keys.any_lo, k_end = keys.any_hi;
-    if (a.splits > 1) {
-        const int groups = (k_end - k_first + 31) / 32, per = (groups + a.splits - 1) / a.splits;
-        const int s0 = min(split * per, groups), s1 = min(s0 + per, groups);
-        k_end = min(k_end, k_first + s1 * 32);
-        k_first += s0 * 32;
-    }
+    split_keys<32>(split, a.splits, k_first, k_end);
     float qf[D / 2];
     load_fragment<D>(qf, row_ptr(a.Q, b, q, h, 4), hf);
     f32x16_t acc[D / 32];
@@ -242,9 +237,9 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     __shared__ __align__(16) float smem[2 * TILE];
     __shared__ int words[8];
     const int tiles = (a.M + 127) / 128;
-    const DensePiece piece = dense_piece(a.B * tiles, a.Hkv);
+    const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
     if (piece.rank < 0) return;
-    const DenseTask task = dense_task(piece.rank, 1, tiles, a.order_q);
+    const DenseTask task = dense_task(piece.rank, a.splits, tiles, a.order_q);
     const int tile = task.tile, b = task.b, hk = piece.head, bh = b * a.Hkv + hk;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hf = lane >> 5;
     const int m = tile * 128 + wave * 32 + l32, mc = min(m, a.M - 1), q = query_of(a, mc), h = hk * a.G + (mc - q * a.G);
@@ -254,6 +249,8 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     const float lse2 = info.lse2[mc & 31], nd = info.ndelta[mc & 31], slope2 = BIAS ? info.slope2[mc & 31] : 0.f;
     const int pos = BIAS ? info.pos[mc & 31] : 0;
     const Keys keys = tile_keys<4>(lo, hi, wave, lane, words);
+    int k_first = keys.any_lo, k_end = keys.any_hi;
+    split_keys<32>(task.split, a.splits, k_first, k_end);
     float qf[D / 2], dof[D / 2];
     load_fragment<D>(qf, row_ptr(a.Q, b, q, h, 4), hf);
     load_fragment<D>(dof, row_ptr(a.dO, b, q, h, 4), hf);
@@ -268,20 +265,20 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
         sk.load([&](int r) { return kbase + min(kb + r, a.Sk - 1) * kss; });
         sv.load([&](int r) { return vbase + min(kb + r, a.Sk - 1) * vss; });
     };
-    if (keys.any_lo < keys.any_hi) fetch(keys.any_lo);
-    for (int kb = keys.any_lo; kb < keys.any_hi; kb += 32) {
+    if (k_first < k_end) fetch(k_first);
+    for (int kb = k_first; kb < k_end; kb += 32) {
         __syncthreads();
         sk.store(smem);
         sv.store(smem + TILE);
         __syncthreads();
-        if (kb + 32 < keys.any_hi) fetch(kb + 32);
-        const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi;
+        if (kb + 32 < k_end) fetch(kb + 32);
+        const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi || kb + 32 > k_end;
         f32x16_t s = over_channels<D>(smem, qf, zero16, l32, hf), dp;
 #pragma unroll
         for (int v = 0; v < 16; ++v) dp[v] = nd;
         dp = over_channels<D>(smem + TILE, dof, dp, l32, hf);
         const float rel = BIAS ? (float)(pos - kb - 4 * hf) : 0.f;
-        const int first_key = lo - kb - 4 * hf, end = hi - kb - 4 * hf;
+        const int first_key = lo - kb - 4 * hf, end = min(hi, k_end) - kb - 4 * hf;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int key = 8 * (v >> 2) + (v & 3);
@@ -291,7 +288,9 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
         }
         over_rows<D>(smem, s, acc, l32, hf, masked, found);
     }
-    if (m < a.M) store_row<D>(const_cast<char*>(row_ptr(a.dQ, b, q, h, 4)), acc, a.scale, hf);
+    if (m < a.M)
+        store_row<D>(a.splits > 1 ? (char*)(a.part_o + (((long long)task.split * a.B * a.Hkv + bh) * a.M + m) * D) : const_cast<char*>(row_ptr(a.dQ, b, q, h, 4)),
+                     acc, a.scale, hf);
 }
 
 template <int D, bool CAP, bool BIAS>
@@ -390,13 +389,16 @@ void launch_fwd(bool cap, hipStream_t st, const DenseArgs& a) {
 #undef LAUNCH
 }
 template <int D>
-void launch_bwd(bool cap, hipStream_t st, const DenseArgs& a) {
-    const dim3 gq(dense_grid((int64_t)a.B * ceil_div64(a.M, 128), a.Hkv)), gk(dense_grid((int64_t)a.B * ceil_div64(a.Sk, 128) * a.splits, a.Hkv)), block(256);
-#define LAUNCH(CAP, BIAS)                                            \
-    do {                                                             \
-        dense_dq_f32_kernel<D, CAP, BIAS><<<gq, block, 0, st>>>(a);  \
-        dense_dkv_f32_kernel<D, CAP, BIAS><<<gk, block, 0, st>>>(a); \
-    } while (0)
+void launch_dq(bool cap, hipStream_t st, const DenseArgs& a) {
+    const dim3 grid(dense_grid((int64_t)a.B * ceil_div64(a.M, 128) * a.splits, a.Hkv)), block(256);
+#define LAUNCH(CAP, BIAS) dense_dq_f32_kernel<D, CAP, BIAS><<<grid, block, 0, st>>>(a)
+    BY_SCORES(LAUNCH);
+#undef LAUNCH
+}
+template <int D>
+void launch_dkv(bool cap, hipStream_t st, const DenseArgs& a) {
+    const dim3 grid(dense_grid((int64_t)a.B * ceil_div64(a.Sk, 128) * a.splits, a.Hkv)), block(256);
+#define LAUNCH(CAP, BIAS) dense_dkv_f32_kernel<D, CAP, BIAS><<<grid, block, 0, st>>>(a)
     BY_SCORES(LAUNCH);
 #undef LAUNCH
 }
@@ -408,4 +410,5 @@ void launch_dense_fwd_f32(int D, bool cap, hipStream_t st, const DenseArgs& a) {
     if (D == 128) few ? launch_fwd<128, 1>(cap, st, a) : launch_fwd<128, 4>(cap, st, a);
     else few ? launch_fwd<64, 1>(cap, st, a) : launch_fwd<64, 4>(cap, st, a);
 }
-void launch_dense_bwd_f32(int D, bool cap, hipStream_t st, const DenseArgs& a) { D == 128 ? launch_bwd<128>(cap, st, a) : launch_bwd<64>(cap, st, a); }
+void launch_dense_dq_f32(int D, bool cap, hipStream_t st, const DenseArgs& a) { D == 128 ? launch_dq<128>(cap, st, a) : launch_dq<64>(cap, st, a); }
+void launch_dense_dkv_f32(int D, bool cap, hipStream_t st, const DenseArgs& a) { D == 128 ? launch_dkv<128>(cap, st, a) : launch_dkv<64>(cap, st, a); }

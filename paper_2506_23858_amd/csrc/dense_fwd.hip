@@ -113,12 +113,7 @@ __global__ __launch_bounds__(64 * NW, 2) void dense_fwd_kernel(DenseArgs a) {
     if (tid < 2) words[tid] = 0;
     int k_first = __builtin_amdgcn_readfirstlane(any_lo), k_end = __builtin_amdgcn_readfirstlane(any_hi);
     if (k_first >= k_end) k_first = k_end = 0;
-    if (a.splits > 1) {                                      // this split's share of the tile's groups
-        const int groups = (k_end - k_first + GK - 1) / GK, per = (groups + a.splits - 1) / a.splits;
-        const int s0 = min(split * per, groups), s1 = min(s0 + per, groups);
-        k_end = min(k_end, k_first + s1 * GK);
-        k_first += s0 * GK;
-    }
+    split_keys<GK>(split, a.splits, k_first, k_end);
     all_hi = min(all_hi, k_end);
     const int n_groups = (k_end - k_first + GK - 1) / GK;
 

@@ -100,13 +100,30 @@ __device__ __forceinline__ float reduce(float x, float* lds) {
 
 template <int NC, int VEC, int L>
 __device__ __forceinline__ void load_weight(const NormArgs& a, int lane, float (&w)[NC][VEC]) {
+    auto load = [&](auto type) {
+        using W = decltype(type);
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c) {
+            const int d0 = (c * L + lane) * VEC;
+            const W* p = (const W*)a.weight + d0;
+            if (d0 + VEC <= a.D) {
+                VecOf<W, VEC> v;
+                __builtin_memcpy(&v, p, sizeof(v));
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const int d = (c * L + lane) * VEC + j;
-            w[c][j] = d >= a.D ? 0.f : !a.weight ? 1.f : a.weight_bf16 ? (float)((const __bf16*)a.weight)[d] : ((const float*)a.weight)[d];
+                for (int j = 0; j < VEC; ++j) w[c][j] = (float)v.v[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) w[c][j] = d0 + j < a.D ? (float)p[j] : 0.f;
+            }
         }
+    };
+    if (a.weight && a.weight_bf16) load(__bf16{});
+    else if (a.weight) load(float{});
+    else
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) w[c][j] = (c * L + lane) * VEC + j < a.D ? 1.f : 0.f;
 }
 struct RowAt { int b, h, s; };
 __device__ __forceinline__ RowAt row_at(long long r, const NormArgs& a) {      // rows in the order (b, s, h)

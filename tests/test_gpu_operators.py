@@ -363,13 +363,14 @@ def test_dense_gradient_by_differences():
 
 def test_dense_streams_graphs_and_repeats():
     Q, K, V, dO = tensors(1, 4, 2, 300, 300, 128, BF16)
-    first = run(Q, K, V, dO)
-    again = run(Q, K, V, dO)
+    every = int32([[0] * 300]), int32([[300] * 300])
+    first = run(Q, K, V, dO, *every)
+    again = run(Q, K, V, dO, *every)
     assert all(torch.equal(first[k], again[k]) for k in first)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        other = run(Q, K, V, dO)
+        other = run(Q, K, V, dO, *every)
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(first[k], other[k]) for k in first)
     B, Sq, Hq, D = Q.shape
@@ -391,7 +392,7 @@ def test_dense_streams_graphs_and_repeats():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(first[k], out[k]) for k in first)
-        assert torch.equal(run(Q, K, V, dO)["dK"], first["dK"])
+        assert torch.equal(run(Q, K, V, dO, *every)["dK"], first["dK"])
 
 
 # ---------------------------------------------------------------------------------------------------------------- together
