@@ -360,7 +360,7 @@ int vmoba_key_ranges(int B, int64_t Sq, int64_t Sk, const int32_t* doc_off, int6
  * s - slopes[h] * |p - j| for query head h, query position p and key position j (positions as in vmoba_key_ranges). */
 typedef struct {
     float softmax_scale;     /* finite */
-    float cap;               /* 0: none; otherwise positive and finite */
+    float cap;               /* 0: none; otherwise positive, at most 4096 (bfloat16: scores are off by up to cap * 2^-22) or 1e30 (float32) */
     const float* slopes;     /* device float32 [Hq], finite, or null: constants, they get no gradient */
     const int32_t* key_lo;   /* device int32 [B][Sq], both or neither: query r reads keys lo <= j < hi (clamped to 0 .. Sk); */
     const int32_t* key_hi;   /* lo >= hi: none.  Null: every query reads every key.  Any ranges, not only those of vmoba_key_ranges */
@@ -368,7 +368,8 @@ typedef struct {
     int64_t q_first;         /* without q_pos query r stands at q_first + r */
 } vmoba_scores;
 
-/* Bytes of workspace of vmoba_dense_fwd (op = VMOBA_OP_ATTN_FWD) and vmoba_dense_bwd (VMOBA_OP_ATTN_BWD); 0: not supported. */
+/* Bytes of workspace of vmoba_dense_fwd (op = VMOBA_OP_ATTN_FWD) and vmoba_dense_bwd (VMOBA_OP_ATTN_BWD); 0: not supported.  Nothing in it outlives a call, so both directions
+ * and all layers can share one; calls that run at the same time, graphs that are replayed at the same time among them, need one each. */
 size_t vmoba_dense_workspace_bytes(int op, int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, int dtype);
 
 /*

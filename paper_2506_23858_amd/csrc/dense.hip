@@ -224,7 +224,7 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
         if (m >= a.M) k = make_int2(0, 0);
         if (k.x >= k.y || lse2 == -INFINITY) lse2 = INFINITY;
         else if (!(fabsf(d) < INFINITY)) lse2 = NAN;
-        info->lse2[r] = lse2;
+        info->c2[r] = (sizeof(T) == 2 && a.cap2 > 0.f ? a.cap2 : 0.f) - lse2;
         info->ndelta[r] = m < a.M && fabsf(d) < INFINITY ? -d : 0.f;
         info->lo[r] = k.x;
         info->hi[r] = k.y;
@@ -318,6 +318,7 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
     if ((how->key_lo != nullptr) != (how->key_hi != nullptr)) return VMOBA_ERR_INVALID_ARG;
     if (how->q_first < INT32_MIN || how->q_first + Sq > INT32_MAX) return VMOBA_ERR_INVALID_ARG;
     if (K->dtype != Q->dtype || V->dtype != Q->dtype || O->dtype != Q->dtype) return VMOBA_ERR_UNSUPPORTED;
+    if (how->cap > (Q->dtype == VMOBA_BF16 ? 4096.f : 1e30f)) return VMOBA_ERR_UNSUPPORTED;
     if (!sizes_of(B, Hq, Hkv, Sq, Sk, D, how->key_lo != nullptr && Q->dtype == VMOBA_F32, z)) return VMOBA_ERR_UNSUPPORTED;
     if (!reach_ok(K, Sk) || !reach_ok(V, Sk)) return VMOBA_ERR_UNSUPPORTED;
     a.Q = make_view(Q);
@@ -345,8 +346,8 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
     a.negate = how->softmax_scale < 0.f ? 0x80008000u : 0u;
     if (how->cap > 0.f) {
         a.cap2 = how->cap * DENSE_LOG2E;
-        a.cap_in = 2.f * a.scale_log2 / how->cap;
-        a.cap_arg = magnitude / how->cap;
+        a.cap_in = std::min(2.f * a.scale_log2 / how->cap, FLT_MAX);      // (finite, so that a score of 0 stays 0)
+        a.cap_arg = std::min(magnitude / how->cap, FLT_MAX);
     }
     return VMOBA_OK;
 }

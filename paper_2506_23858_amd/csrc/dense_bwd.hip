@@ -2,7 +2,7 @@
 // kernel owns rows and walks their keys (S, dP, dQ: three products), the dK/dV kernel owns keys and walks the rows that read
 // them (S, dP, dV, dK: four).  Seven products for the five that a single pass with dQ in atomics would need.
 //
-// dz = P (dP - delta) (1 - tanh^2), rounded to bfloat16 for the products that follow (relative error 2^-9 a value, like P's).
+// dz = P (dP - delta) (1 - tanh^2), 1 - tanh^2 = 4 (r - r^2), rounded to bfloat16 for the products that follow (relative error 2^-9 a value, like P's).
 // Masked pairs: their scores are replaced (-inf, or 0 with an infinite log-sum-exp), so P and dz are 0.  A masked value that is not finite would still spoil a sum -- 0 times
 // infinity is no number --, so tiles that pass the last key or hold rows without keys lose such values in LDS before they are multiplied, and a
 // workgroup whose sums end up not finite starts again with all tiles cleaned so.  A pair that does read such a value has a log-sum-exp or a delta that is not
@@ -11,15 +11,16 @@
 
 namespace {
 
-// x = <q, k> -> weight P, from c = -(log-sum-exp + bias), base 2; f: what P (dP - delta) is multiplied by (CAP alone).
+// x = <q, k> -> weight P, from c2 = -(log-sum-exp + bias), base 2, with the cap + cap2 (see RowInfo); f (cap alone): a quarter of what P (dP - delta) is multiplied
+// by, r - r^2; the 4 is in the factor that the sums end with.
 template <bool CAP>
-__device__ __forceinline__ float weight_of(const DenseArgs& a, float x, float c, float& f) {
+__device__ __forceinline__ float weight_of(const DenseArgs& a, float x, float c2, float& f) {
     if constexpr (CAP) {
         const float r = __builtin_amdgcn_rcpf(1.f + exp2_raw(x * a.cap_in));
-        f = r * fmaf(-4.f, r, 4.f);
-        return exp2_raw(fmaf(-2.f * a.cap2, r, a.cap2 + c));
+        f = fmaf(-r, r, r);
+        return exp2_raw(fmaf(-2.f * a.cap2, r, c2));
     } else {
-        return exp2_raw(fmaf(x, a.scale_log2, c));
+        return exp2_raw(fmaf(x, a.scale_log2, c2));
     }
 }
 
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
     const RowInfo* info = reinterpret_cast<const RowInfo*>(a.row_info) + (long long)bh * ((a.M + 31) / 32);
 
     int lo[2], hi[2], row_pos[2];
-    float lse2[2], slope2[2];
+    float c2[2], slope2[2];
     f32x4_t ndl[2];
     bf16x8_t qf[2][KSTEPS], dof[2][KSTEPS];
 #pragma unroll
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
         const RowInfo& r = info[mc >> 5];
         lo[t] = m < a.M ? r.lo[mc & 31] : 0;
         hi[t] = m < a.M ? r.hi[mc & 31] : 0;
-        lse2[t] = r.lse2[mc & 31];
+        c2[t] = r.c2[mc & 31];
         const float d = r.ndelta[mc & 31];
         ndl[t] = f32x4_t{d, d, d, d};
         slope2[t] = BIAS ? r.slope2[mc & 31] : 0.f;
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(256, 2) void dense_dq_kernel(DenseArgs a) {
         any_hi = max(any_hi, some ? hi[t] : 0);
         all_lo = max(all_lo, some ? lo[t] : 0);
         all_hi = min(all_hi, some ? hi[t] : INT32_MAX);
-        if (m0 + 16 * t + l16 >= a.M) lse2[t] = INFINITY;
+        if (m0 + 16 * t + l16 >= a.M) c2[t] = -INFINITY;
     }
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) {
@@ -171,9 +172,8 @@ again:
                 for (int t = 0; t < 2; ++t) rel[t] = BIAS ? (float)(row_pos[t] - kb - 4 * g) : 0.f;
                 auto p_value = [&](int v) {           // S^T -> P^T (1 - tanh^2), in place
                     const int kt = v >> 3, t = (v >> 2) & 1, i = v & 3;
-                    float f = 1.f, c2 = -lse2[t];
-                    if constexpr (BIAS) c2 = fmaf(-slope2[t], fabsf(rel[t] - (float)(16 * kt + i)), c2);
-                    float p = weight_of<CAP>(a, s[kt][t][i], c2, f);
+                    float f = 1.f;
+                    float p = weight_of<CAP>(a, s[kt][t][i], BIAS ? fmaf(-slope2[t], fabsf(rel[t] - (float)(16 * kt + i)), c2[t]) : c2[t], f);
                     if constexpr (CAP) p *= f;
                     s[kt][t][i] = p;
                 };
@@ -247,6 +247,7 @@ again:
             goto again;
         }
     }
+    const float out = CAP ? 4.f * a.scale : a.scale;
     if (a.splits > 1) {                         // this split's sums, added up by dense_sum_kernel
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -254,7 +255,7 @@ again:
             if (m < a.M) {
                 float* dst = a.part_o + (((long long)task.split * a.B * a.Hkv + bh) * a.M + m) * D + 4 * g;
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<f32x4_t*>(dst + 16 * ct) = acc[ct][t] * a.scale;
+                for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<f32x4_t*>(dst + 16 * ct) = acc[ct][t] * out;
             }
         }
         return;
@@ -265,8 +266,8 @@ again:
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             u32x2_t v;
-            v.x = pack_bf16x2(acc[ct][t][0] * a.scale, acc[ct][t][1] * a.scale);
-            v.y = pack_bf16x2(acc[ct][t][2] * a.scale, acc[ct][t][3] * a.scale);
+            v.x = pack_bf16x2(acc[ct][t][0] * out, acc[ct][t][1] * out);
+            v.y = pack_bf16x2(acc[ct][t][2] * out, acc[ct][t][3] * out);
             *reinterpret_cast<u32x2_t*>(mine + (t * 16 + l16) * OPITCH + (ct * 16 + g * 4) * 2) = v;
         }
     __builtin_amdgcn_s_waitcnt(0xC07F);
@@ -385,21 +386,21 @@ again:
         unsigned pw[2][4];                                // P as packed pairs
         auto p_pair = [&](int j) {                        // values 2 j and 2 j + 1: S -> P (packed), P (1 - tanh^2) in its place
             const int t = j >> 2, kt = (j >> 1) & 1, i0 = (j & 1) * 2, r0 = 16 * t + 4 * g + i0, key = kw + 16 * kt + l16;
-            f32x2_t l2 = *reinterpret_cast<const f32x2_t*>(ri->lse2 + r0);
+            f32x2_t c2 = *reinterpret_cast<const f32x2_t*>(ri->c2 + r0);
             float p[2];
             if (__builtin_expect(masked, 0)) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     if (one_range ? !reads[kt] : key < ri->lo[r0 + e] || key >= ri->hi[r0 + e]) {
                         s[t][kt][i0 + e] = 0.f;
-                        l2[e] = INFINITY;
+                        c2[e] = -INFINITY;
                     }
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float f = 1.f, c2 = -l2[e];
-                if constexpr (BIAS) c2 = fmaf(-ri->slope2[r0 + e], fabsf((float)(ri->pos[r0 + e] - key)), c2);
-                p[e] = weight_of<CAP>(a, s[t][kt][i0 + e], c2, f);
+                float f = 1.f;
+                if constexpr (BIAS) c2[e] = fmaf(-ri->slope2[r0 + e], fabsf((float)(ri->pos[r0 + e] - key)), c2[e]);
+                p[e] = weight_of<CAP>(a, s[t][kt][i0 + e], c2[e], f);
                 s[t][kt][i0 + e] = CAP ? p[e] * f : p[e];
             }
             pw[kt][2 * t + (j & 1)] = pack_bf16x2(p[0], p[1]);
@@ -505,6 +506,7 @@ again:
             goto again;
         }
     }
+    const float scale_k = CAP ? 4.f * a.scale : a.scale;
     if (a.splits > 1) {                                   // this split's sums, added up by dense_sum_kernel
         const long long n = (long long)a.B * a.Hkv * a.Sk;
 #pragma unroll
@@ -514,7 +516,7 @@ again:
                 float* dst = a.part_o + (2 * task.split * n + (long long)bh * a.Sk + key) * D + 4 * g;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    *reinterpret_cast<f32x4_t*>(dst + 16 * ct) = dk[ct][kt] * a.scale;
+                    *reinterpret_cast<f32x4_t*>(dst + 16 * ct) = dk[ct][kt] * scale_k;
                     *reinterpret_cast<f32x4_t*>(dst + n * D + 16 * ct) = dv[ct][kt];
                 }
             }
@@ -525,7 +527,7 @@ again:
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         const TensorView& out = which == 0 ? a.dV : a.dK;
-        const float f = which == 0 ? 1.f : a.scale;
+        const float f = which == 0 ? 1.f : scale_k;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll

@@ -34,8 +34,8 @@ struct DenseArgs {
 
 // What the dK/dV kernel needs to know of 32 consecutive rows, one 1 KB request: arrays of 32 words.
 struct RowInfo {
-    float lse2[32];        // log-sum-exp of the row, base 2; +inf for a row without keys (all its weights are then 0), NaN for a row whose delta is
-                           // not finite (its weights are then NaN)
+    float c2[32];          // -(log-sum-exp of the row, base 2), bfloat16 calls with a cap: + cap2; -inf for a row without keys (all its weights are then
+                           // 0), NaN for a row whose delta is not finite (its weights are then NaN)
     float ndelta[32];      // -rowsum(dO * O), finite
     int lo[32], hi[32];    // its keys
     float slope2[32];      // slope * log2(e)

@@ -224,10 +224,10 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
 
 // P and dz of one pair from x = <q, k> and dp = dP - delta.
 template <bool CAP>
-__device__ __forceinline__ void pair_gradient(const DenseArgs& a, float x, float scl, float bias2, float lse2, float dp, float& p, float& dz) {
+__device__ __forceinline__ void pair_gradient(const DenseArgs& a, float x, float scl, float bias2, float c2, float dp, float& p, float& dz) {
     float t = 0.f;
     const float s2 = score32<CAP>(a, x, scl, t);
-    p = exp2_raw(CAP ? s2 - bias2 - lse2 : fmaf(x, scl, -bias2 - lse2));
+    p = exp2_raw(CAP ? s2 - bias2 + c2 : fmaf(x, scl, c2 - bias2));
     dz = p * dp * (CAP ? 1.f - t * t : 1.f);
 }
 
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     const float scl = a.negate ? -a.scale_log2 : a.scale_log2;
     const RowInfo& info = (reinterpret_cast<const RowInfo*>(a.row_info) + (long long)bh * ((a.M + 31) / 32))[mc >> 5];
     const int lo = m < a.M ? info.lo[mc & 31] : 0, hi = m < a.M ? info.hi[mc & 31] : 0;
-    const float lse2 = info.lse2[mc & 31], nd = info.ndelta[mc & 31], slope2 = BIAS ? info.slope2[mc & 31] : 0.f;
+    const float c2 = info.c2[mc & 31], nd = info.ndelta[mc & 31], slope2 = BIAS ? info.slope2[mc & 31] : 0.f;
     const int pos = BIAS ? info.pos[mc & 31] : 0;
     const Keys keys = tile_keys<4>(lo, hi, wave, lane, words);
     int k_first = keys.any_lo, k_end = keys.any_hi;
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
         for (int v = 0; v < 16; ++v) {
             const int key = 8 * (v >> 2) + (v & 3);
             float p, dz;
-            pair_gradient<CAP>(a, s[v], scl, BIAS ? slope2 * fabsf(rel - (float)key) : 0.f, lse2, dp[v], p, dz);
+            pair_gradient<CAP>(a, s[v], scl, BIAS ? slope2 * fabsf(rel - (float)key) : 0.f, c2, dp[v], p, dz);
             s[v] = masked && (key < first_key || key >= end) ? 0.f : dz;
         }
         over_rows<D>(smem, s, acc, l32, hf, masked, found);
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
         for (int v = 0; v < 16; ++v) {
             const int r = 8 * (v >> 2) + 4 * hf + (v & 3);
             float p, dz;
-            pair_gradient<CAP>(a, s[v], scl, BIAS ? ri.slope2[r] * fabsf((float)(ri.pos[r] - key)) : 0.f, ri.lse2[r], dp[v], p, dz);
+            pair_gradient<CAP>(a, s[v], scl, BIAS ? ri.slope2[r] * fabsf((float)(ri.pos[r] - key)) : 0.f, ri.c2[r], dp[v], p, dz);
             if (masked) {
                 const bool reads = key >= ri.lo[r] && key < ri.hi[r];
                 p = reads ? p : 0.f;

@@ -181,10 +181,13 @@ again:
         // product x -> kept score, of 16 keys kt of the group at kb
         auto keep_score = [&](f32x4_t(&s)[2][QT], int kt, int t, int i, int kb) {
             if constexpr (CAP || BIAS) {
-                float r, v = dense_score<CAP>(a, s[kt][t][i], r);
-                if constexpr (BIAS) v = fmaf(-slope2[t], fabsf((float)(row_pos[t] - kb - 4 * g) - (float)(16 * kt + i)), v);
-                else v = -r;
-                s[kt][t][i] = v;
+                if constexpr (BIAS) {
+                    float r;
+                    const float v = dense_score<CAP>(a, s[kt][t][i], r);
+                    s[kt][t][i] = fmaf(-slope2[t], fabsf((float)(row_pos[t] - kb - 4 * g) - (float)(16 * kt + i)), v);
+                } else {
+                    s[kt][t][i] = __builtin_amdgcn_rcpf(-1.f - exp2_raw(s[kt][t][i] * a.cap_in));
+                }
             }
         };
 

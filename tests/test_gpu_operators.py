@@ -273,7 +273,7 @@ def test_key_ranges_of_single_queries_and_bad_offsets():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("scale,cap", [(-0.2, 0.0), (0.0, 0.0), (-0.2, 3.0), (0.0, 3.0), (40.0, 0.0)])
+@pytest.mark.parametrize("scale,cap", [(-0.2, 0.0), (0.0, 0.0), (-0.2, 3.0), (0.0, 3.0), (40.0, 0.0), (0.2, 4096.0), (0.2, 1e-30)])
 def test_dense_scales_of_any_sign(dtype, scale, cap):
     Q, K, V, dO = tensors(1, 2, 1, 70, 70, 64, dtype, scale=0.5)
     lo, hi = (torch.empty(1, 70, dtype=torch.int32, device="cuda") for _ in range(2))
@@ -393,6 +393,38 @@ def test_dense_streams_graphs_and_repeats():
         torch.cuda.synchronize()
         assert all(torch.equal(first[k], out[k]) for k in first)
         assert torch.equal(run(Q, K, V, dO, *every)["dK"], first["dK"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Hq,Sq", [(300, 1), (300, 3), (255, 2)])
+def test_dense_many_heads_on_one_key_head(Hq, Sq, dtype):
+    check(*tensors(1, Hq, 1, Sq, 70, 64, dtype), slopes=torch.linspace(0.0, 0.1, Hq, device="cuda"), q_first=70 - Sq)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_dense_strides_and_orders(dtype):
+    """Head-major tensors, tensors with rows further apart than they are long, keys and values that all batch elements share."""
+    B, Hq, Hkv, Sq, Sk, D = 2, 4, 2, 50, 90, 64
+    Q = ou.normal(1, (B, Hq, Sq, D), dtype).transpose(1, 2)
+    K = ou.normal(2, (1, Sk, Hkv, D), dtype).expand(B, -1, -1, -1)
+    V = ou.normal(3, (1, Hkv, Sk, 2 * D), dtype).transpose(1, 2)[..., :D].expand(B, -1, -1, -1)
+    dO = ou.normal(4, (B, Sq, D // 8, Hq, 16), dtype)[:, :, 2:6].reshape(B, Sq, Hq, D)
+    check(Q, K, V, dO)
+
+
+def test_dense_cache_beyond_32_bit_offsets():
+    """Three caches of 2 GiB each for keys and for values: the last keys of the last one."""
+    B, H, S, D, n = 3, 8, 1 << 20, 128, 300
+    K, V = (torch.empty(B, S, H, D, dtype=BF16, device="cuda") for _ in range(2))
+    tail = ou.normal(1, (2, n, H, D), BF16)
+    K[2, S - n:], V[2, S - n:] = tail[0], tail[1]
+    Q = ou.normal(2, (B, 1, H, D), BF16)
+    lo, hi = int32([[0], [0], [S - n]]), int32([[0], [0], [S]])
+    got = run(Q, K, V, None, lo, hi, bwd=False)
+    ref = ou.attention(Q[2:], tail[:1], tail[1:], int32([[0]]), int32([[n]]), None, 1 / math.sqrt(D))
+    ou.within("O", got["O"][2:], *ref["O"])
+    ou.within("LSE", got["LSE"][2:], *ref["LSE"])
+    assert bool((got["O"][:2] == 0).all())
 
 
 # ---------------------------------------------------------------------------------------------------------------- together

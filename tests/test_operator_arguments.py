@@ -122,7 +122,7 @@ BOTH = [
     (dict(B=0), INVALID), (dict(Hq=0), INVALID), (dict(Hkv=0), INVALID), (dict(Hkv=3), INVALID), (dict(Sq=0), INVALID), (dict(Sk=0), INVALID), (dict(D=96), UNSUPPORTED),
     (dict(Sk=1 << 24), UNSUPPORTED), (dict(Sq=1 << 23), UNSUPPORTED), (dict(Q=None), INVALID), (dict(K=desc(P + 8)), INVALID), (dict(V=desc(s=1001)), INVALID),
     (dict(K=desc(dtype=vb.VMOBA_F32)), UNSUPPORTED), (dict(O=desc(dtype=vb.VMOBA_F32)), UNSUPPORTED), (dict(Q=desc(dtype=vb.VMOBA_F8E4M3)), INVALID), (dict(K=desc(s=-1024)), UNSUPPORTED),
-    (dict(K=desc(s=1 << 22)), UNSUPPORTED), (dict(Sk=1 << 22, K=desc(s=1 << 10)), UNSUPPORTED), (dict(scale=math.nan), INVALID), (dict(cap=-1.0), INVALID), (dict(cap=math.inf), INVALID),
+    (dict(K=desc(s=1 << 22)), UNSUPPORTED), (dict(Sk=1 << 22, K=desc(s=1 << 10)), UNSUPPORTED), (dict(scale=math.nan), INVALID), (dict(cap=-1.0), INVALID), (dict(cap=math.inf), INVALID), (dict(cap=4097.0), UNSUPPORTED),
     (dict(lo=P), INVALID), (dict(hi=P), INVALID), (dict(first=1 << 31), INVALID), (dict(LSE=None), INVALID), (dict(ws=None), INVALID), (dict(ws=P + 16), INVALID), (dict(size=255), WORKSPACE)]
 
 
