@@ -46,31 +46,31 @@ __global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
     const long long n = (long long)a.B * a.Hkv * a.M, i = ((long long)blockIdx.x * 256 + threadIdx.x) / LPR;
     const int part = threadIdx.x % LPR;
     if (i >= n) return;
-    constexpr int MB = 8;                                    // splits in flight
-    float top = -INFINITY;
-    for (int s0 = 0; s0 < a.splits; s0 += MB) {
-        float l[MB];
-#pragma unroll
-        for (int u = 0; u < MB; ++u) l[u] = a.part_lse[min(s0 + u, a.splits - 1) * n + i];
-#pragma unroll
-        for (int u = 0; u < MB; ++u) top = l[u] > top || l[u] != l[u] ? l[u] : top;      // (a NaN stays)
-    }
+    // one pass with a running maximum, MB splits in flight
+    constexpr int MB = 16;
+    float top = -INFINITY, sum = 0.f;
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int s0 = 0; s0 < a.splits && top != -INFINITY; s0 += MB) {
-        float w[MB];
+    for (int s0 = 0; s0 < a.splits; s0 += MB) {
+        float l[MB], before = top;
         f32x4_t x[MB];
 #pragma unroll
         for (int u = 0; u < MB; ++u) {
             const long long at = min(s0 + u, a.splits - 1) * n + i;
-            w[u] = s0 + u < a.splits ? exp2_raw(a.part_lse[at] - top) : 0.f;
+            l[u] = s0 + u < a.splits ? a.part_lse[at] : -INFINITY;
             x[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + part * 4);
         }
 #pragma unroll
+        for (int u = 0; u < MB; ++u) top = l[u] > top || l[u] != l[u] ? l[u] : top;      // (a NaN stays)
+        if (top == -INFINITY) continue;
+        const float alpha = exp2_raw(before - top);
+        sum *= alpha;
+        acc *= alpha;
+#pragma unroll
         for (int u = 0; u < MB; ++u) {
-            if (w[u] == 0.f) continue;                       // a split without keys of this row
-            sum += w[u];
-            acc += x[u] * w[u];
+            const float w = exp2_raw(l[u] - top);
+            if (w == 0.f) continue;                          // a split without keys of this row
+            sum += w;
+            acc += x[u] * w;
         }
     }
     const float inv = top == -INFINITY ? 0.f : 1.f / sum;
