@@ -5,7 +5,7 @@
 //   * over channels, lane half hf takes channels hf * D/2 + t at step t: both operands are runs of a row, 16 bytes at a time;
 //   * over 32 keys (or rows), step 4 * i + r takes keys 8 * i + 4 * hf + r: the accumulator value itself is the B operand, and A is a
 //     column of the tile, 32 consecutive floats of two rows.
-// Tiles of 32 rows go through registers to LDS, requested one tile ahead, in rows padded by 16 bytes.  One such instruction is 64 cycles of the
+// Tiles of 32 rows go through registers to LDS, requested one tile ahead, in rows padded by 16 bytes and in two buffers, so that a tile is one barrier.  One such instruction is 64 cycles of the
 // matrix pipe for one LDS read of 4 or a quarter of one of 16 bytes: the pipe is what bounds these kernels.
 #include "dense_common.h"
 
@@ -49,20 +49,20 @@ __device__ __forceinline__ f32x16_t over_channels(const float* tile, const float
     }
     return acc;
 }
-// acc[dt] += (tile columns 32 * dt + l32)^T . p over the tile's 32 rows; CLEAN: values that are not finite count as 0.
+// acc[dt] += (tile columns 32 * dt + l32)^T . p over the tile's 32 rows.  Values of the classes `special` count as 0: NOT_FINITE where a
+// mask cuts the tile (their weight of 0 would make them NaNs), none elsewhere.  A test and a selection in the shadow of the matrix
+// instruction: with a branch at each value instead, and one tile buffer, 8192 tokens x 8 heads x 128 channels took 2.68 ms (now 2.27)
+// forward and 10.0 (8.7) backward.
+constexpr int NOT_FINITE = 0x207;                            // classes of a float: NaNs, -inf, +inf
 template <int D>
-__device__ __forceinline__ void over_rows(const float* tile, const f32x16_t& p, f32x16_t (&acc)[D / 32], int l32, int hf, bool clean, unsigned& found) {
+__device__ __forceinline__ void over_rows(const float* tile, const f32x16_t& p, f32x16_t (&acc)[D / 32], int l32, int hf, int special) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
         const float* row = tile + (8 * (v >> 2) + 4 * hf + (v & 3)) * PITCH<D> + l32;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) {
-            float x = row[32 * dt];
-            if (clean && !(fabsf(x) < INFINITY)) {
-                x = 0.f;
-                found = 1u;
-            }
-            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[v], acc[dt], 0, 0, 0);
+            const float x = row[32 * dt];
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_amdgcn_classf(x, special) ? 0.f : x, p[v], acc[dt], 0, 0, 0);
         }
     }
 }
@@ -134,7 +134,7 @@ __device__ __forceinline__ Keys tile_keys(int lo, int hi, int wave, int lane, in
 template <int D, int NW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) {
     constexpr int NT = 64 * NW, TILE = 32 * PITCH<D>;
-    __shared__ __align__(16) float smem[2 * TILE];
+    __shared__ __align__(16) float smem[2][2 * TILE];
     __shared__ int words[2 * NW];
     const int tiles = (a.M + 32 * NW - 1) / (32 * NW);
     const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
@@ -156,8 +156,9 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
     f32x16_t acc[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16;
+    const float none = CAP || BIAS || scl > 0.f ? -INFINITY : INFINITY;      // stands for a masked score
     float m_run = -3e38f, l_run = 0.f;
-    unsigned found = 0;
+    bool found = false;                                      // values of V that over_rows took out
     const char *kbase = row_ptr(a.K, b, 0, hk, 4), *vbase = row_ptr(a.V, b, 0, hk, 4);
     const long long kss = a.K.stride_s * 4, vss = a.V.stride_s * 4;
     Stage<D, NT> sk, sv;
@@ -165,15 +166,21 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
         sk.load([&](int r) { return kbase + min(kb + r, a.Sk - 1) * kss; });
         sv.load([&](int r) { return vbase + min(kb + r, a.Sk - 1) * vss; });
     };
-    if (k_first < k_end) fetch(k_first);
-    for (int kb = k_first; kb < k_end; kb += 32) {
+    auto place = [&](int buf) {
+        sk.store(smem[buf]);
+        sv.store(smem[buf] + TILE);
+    };
+    if (k_first < k_end) {
+        fetch(k_first);
+        place(0);
+    }
+    int buf = 0;
+    for (int kb = k_first; kb < k_end; kb += 32, buf ^= 1) {
         __syncthreads();
-        sk.store(smem);
-        sv.store(smem + TILE);
-        __syncthreads();
+        const float* tk = smem[buf];
         if (kb + 32 < k_end) fetch(kb + 32);
         const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi || kb + 32 > k_end;
-        f32x16_t s = over_channels<D>(smem, qf, zero16, l32, hf);
+        f32x16_t s = over_channels<D>(tk, qf, zero16, l32, hf);
         const float rel = BIAS ? (float)(pos - kb - 4 * hf) : 0.f;
         const int first_key = lo - kb - 4 * hf, end = min(hi, k_end) - kb - 4 * hf;
         float mx = -INFINITY;
@@ -183,7 +190,23 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
             float t, s2 = score32<CAP>(a, s[v], scl, t);
             if constexpr (BIAS) s2 = fmaf(-slope2, fabsf(rel - (float)key), s2);
             if constexpr (CAP || BIAS) s[v] = s2;
-            if (!masked || (key >= first_key && key < end)) mx = fmaxf(mx, s2);
+            mx = fmaxf(mx, s2);
+        }
+        if (masked) {
+            mx = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int key = 8 * (v >> 2) + (v & 3);
+                s[v] = key >= first_key && key < end ? s[v] : none;
+                mx = fmaxf(mx, CAP || BIAS ? s[v] : s[v] * scl);
+            }
+            const float* half = tk + TILE + l32 * PITCH<D> + hf * (D / 2);
+#pragma unroll
+            for (int t = 0; t < D / 2; t += 4) {
+                const f32x4_t x = *reinterpret_cast<const f32x4_t*>(half + t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) found |= __builtin_amdgcn_classf(x[j], NOT_FINITE);
+            }
         }
         mx = swap_halves_max(mx);
         const float m_new = fmaxf(m_run, mx), alpha = exp2_raw(m_run - m_new);
@@ -191,9 +214,7 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
         l_run *= alpha;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-            const int key = 8 * (v >> 2) + (v & 3);
-            float p = exp2_raw(CAP || BIAS ? s[v] - m_run : fmaf(s[v], scl, -m_run));
-            if (masked && (key < first_key || key >= end)) p = 0.f;
+            const float p = exp2_raw(CAP || BIAS ? s[v] - m_run : fmaf(s[v], scl, -m_run));
             l_run += p;
             s[v] = p;
         }
@@ -203,7 +224,8 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[dt][v] *= alpha;
         }
-        over_rows<D>(smem + TILE, s, acc, l32, hf, masked, found);
+        over_rows<D>(tk + TILE, s, acc, l32, hf, masked ? NOT_FINITE : 0);
+        if (kb + 32 < k_end) place(buf ^ 1);
     }
     const float l = swap_halves_sum(l_run), inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m_run + log2f(l);
     const long long part0 = ((long long)split * a.B * a.Hkv + bh) * a.M;
@@ -216,7 +238,7 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
             if (hf == 0) a.LSE[((long long)b * a.Hq + h) * a.Sq + q] = lse2 * DENSE_LN2;
         }
     }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(found != 0) == 0, 1)) return;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(found) == 0, 1)) return;
     // (rows m0 + 16 + lane % 16 are lanes 16 .. 31)
     dense_repair<float, D, CAP, BIAS>(a, b, hk, m0, lane, part0, k_first, k_end, keys.all_lo, keys.all_hi, lo, __shfl(lo, 16 + (lane & 15), 64), hi,
                                       __shfl(hi, 16 + (lane & 15), 64), lse2, __shfl(lse2, 16 + (lane & 15), 64));
@@ -234,7 +256,7 @@ __device__ __forceinline__ void pair_gradient(const DenseArgs& a, float x, float
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     constexpr int TILE = 32 * PITCH<D>;
-    __shared__ __align__(16) float smem[2 * TILE];
+    __shared__ __align__(16) float smem[2][2 * TILE];
     __shared__ int words[8];
     const int tiles = (a.M + 127) / 128;
     const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
@@ -257,7 +279,6 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     f32x16_t acc[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16;
-    unsigned found = 0;
     const char *kbase = row_ptr(a.K, b, 0, hk, 4), *vbase = row_ptr(a.V, b, 0, hk, 4);
     const long long kss = a.K.stride_s * 4, vss = a.V.stride_s * 4;
     Stage<D, 256> sk, sv;
@@ -265,18 +286,24 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
         sk.load([&](int r) { return kbase + min(kb + r, a.Sk - 1) * kss; });
         sv.load([&](int r) { return vbase + min(kb + r, a.Sk - 1) * vss; });
     };
-    if (k_first < k_end) fetch(k_first);
-    for (int kb = k_first; kb < k_end; kb += 32) {
+    auto place = [&](int buf) {
+        sk.store(smem[buf]);
+        sv.store(smem[buf] + TILE);
+    };
+    if (k_first < k_end) {
+        fetch(k_first);
+        place(0);
+    }
+    int buf = 0;
+    for (int kb = k_first; kb < k_end; kb += 32, buf ^= 1) {
         __syncthreads();
-        sk.store(smem);
-        sv.store(smem + TILE);
-        __syncthreads();
+        const float* tk = smem[buf];
         if (kb + 32 < k_end) fetch(kb + 32);
         const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi || kb + 32 > k_end;
-        f32x16_t s = over_channels<D>(smem, qf, zero16, l32, hf), dp;
+        f32x16_t s = over_channels<D>(tk, qf, zero16, l32, hf), dp;
 #pragma unroll
         for (int v = 0; v < 16; ++v) dp[v] = nd;
-        dp = over_channels<D>(smem + TILE, dof, dp, l32, hf);
+        dp = over_channels<D>(tk + TILE, dof, dp, l32, hf);
         const float rel = BIAS ? (float)(pos - kb - 4 * hf) : 0.f;
         const int first_key = lo - kb - 4 * hf, end = min(hi, k_end) - kb - 4 * hf;
 #pragma unroll
@@ -284,9 +311,17 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
             const int key = 8 * (v >> 2) + (v & 3);
             float p, dz;
             pair_gradient<CAP>(a, s[v], scl, BIAS ? slope2 * fabsf(rel - (float)key) : 0.f, c2, dp[v], p, dz);
-            s[v] = masked && (key < first_key || key >= end) ? 0.f : dz;
+            s[v] = dz;
         }
-        over_rows<D>(smem, s, acc, l32, hf, masked, found);
+        if (masked) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int key = 8 * (v >> 2) + (v & 3);
+                s[v] = key >= first_key && key < end ? s[v] : 0.f;
+            }
+        }
+        over_rows<D>(tk, s, acc, l32, hf, masked ? NOT_FINITE : 0);
+        if (kb + 32 < k_end) place(buf ^ 1);
     }
     if (m < a.M)
         store_row<D>(a.splits > 1 ? (char*)(a.part_o + (((long long)task.split * a.B * a.Hkv + bh) * a.M + m) * D) : const_cast<char*>(row_ptr(a.dQ, b, q, h, 4)),
@@ -296,8 +331,8 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
     constexpr int TILE = 32 * PITCH<D>;
-    __shared__ __align__(16) float smem[2 * TILE];
-    __shared__ RowInfo ri;
+    __shared__ __align__(16) float smem[2][2 * TILE];
+    __shared__ RowInfo infos[2];
     const int tiles = (a.Sk + 127) / 128;
     const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
     if (piece.rank < 0) return;
@@ -315,7 +350,6 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
     f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zero16;
-    unsigned found = 0;
     Stage<D, 256> sq, so;
     uint32_t si = 0;                                         // the thread's word of the row information
     ChunkWalk walk(bounds, n_chunks, k0, k0 + 128, lane, task.split, a.splits);
@@ -330,37 +364,48 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
         so.load(row(a.dO));
         si = reinterpret_cast<const uint32_t*>(info + c)[tid];
     };
+    auto place = [&](int buf) {
+        sq.store(smem[buf]);
+        so.store(smem[buf] + TILE);
+        reinterpret_cast<uint32_t*>(&infos[buf])[tid] = si;
+    };
     int c = walk.next();
-    if (c >= 0) fetch(c);
-    while (c >= 0) {
+    if (c >= 0) {
+        fetch(c);
+        place(0);
+    }
+    for (int buf = 0; c >= 0; buf ^= 1) {
         const int all_lo = walk.all_lo, all_hi = walk.all_hi;
         __syncthreads();
-        sq.store(smem);
-        so.store(smem + TILE);
-        reinterpret_cast<uint32_t*>(&ri)[tid] = si;
-        __syncthreads();
+        const float* tq = smem[buf];
+        const RowInfo& ri = infos[buf];
         c = walk.next();
         if (c >= 0) fetch(c);
         const bool masked = kw < all_lo || kw + 32 > all_hi;
-        f32x16_t s = over_channels<D>(smem, kf, zero16, l32, hf), dp;
+        f32x16_t s = over_channels<D>(tq, kf, zero16, l32, hf), dp;
 #pragma unroll
         for (int v = 0; v < 16; ++v) dp[v] = ri.ndelta[8 * (v >> 2) + 4 * hf + (v & 3)];
-        dp = over_channels<D>(smem + TILE, vf, dp, l32, hf);
+        dp = over_channels<D>(tq + TILE, vf, dp, l32, hf);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int r = 8 * (v >> 2) + 4 * hf + (v & 3);
             float p, dz;
             pair_gradient<CAP>(a, s[v], scl, BIAS ? ri.slope2[r] * fabsf((float)(ri.pos[r] - key)) : 0.f, ri.c2[r], dp[v], p, dz);
-            if (masked) {
-                const bool reads = key >= ri.lo[r] && key < ri.hi[r];
-                p = reads ? p : 0.f;
-                dz = reads ? dz : 0.f;
-            }
             s[v] = p;
             dp[v] = dz;
         }
-        over_rows<D>(smem + TILE, s, dv, l32, hf, masked, found);
-        over_rows<D>(smem, dp, dk, l32, hf, masked, found);
+        if (masked) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int r = 8 * (v >> 2) + 4 * hf + (v & 3);
+                const bool reads = key >= ri.lo[r] && key < ri.hi[r];
+                s[v] = reads ? s[v] : 0.f;
+                dp[v] = reads ? dp[v] : 0.f;
+            }
+        }
+        over_rows<D>(tq + TILE, s, dv, l32, hf, masked ? NOT_FINITE : 0);
+        over_rows<D>(tq, dp, dk, l32, hf, masked ? NOT_FINITE : 0);
+        if (c >= 0) place(buf ^ 1);
     }
     if (key < a.Sk && a.splits > 1) {                        // this split's sums, added up by dense_sum_kernel
         const long long n = (long long)a.B * a.Hkv * a.Sk;
