@@ -244,15 +244,19 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     }
 }
 
-// Splits of a row tile's keys.  Without key ranges: as many pieces as run at a time (two per compute unit), at least 128 keys each; one query
-// of 16 heads on 4 key heads, 8 sequences of 32 760 keys: 32 tiles on 512 places.  With ranges tiles cost different amounts, and the longest of a few that all
+// Splits of a row tile's keys: as many pieces as run at a time (two per compute unit), at least 128 keys each; one query of 16 heads on 4 key
+// heads, 8 sequences of 32 760 keys: 32 tiles on 512 places.  With ranges tiles cost different amounts, and the longest of a few that all
 // run at once decides: for float32 four times as many pieces, at least 256 keys each, unless there are so many tiles that their order evens them out (2 x 2001 tokens, 16 heads on
 // 4, 64 channels, causal, forward and backward: 1450 -> 900 us).  bfloat16 keeps to one round: its groups of keys take a quarter of the time, and pieces' ends
 // cost as much (1637 tokens x 12 heads, causal: 49 us, 74 with four times the pieces).
-int splits_for(int64_t tiles, int64_t Sk, bool uneven) {
-    const int64_t pieces = uneven && tiles <= 640 ? 2048 : 512, by_places = pieces / std::max<int64_t>(tiles, 1), by_keys = ceil_div64(Sk, uneven ? 256 : 128);
+int splits_for(int64_t tiles, int64_t Sk, bool uneven, int64_t places) {
+    const int64_t pieces = uneven && tiles <= 640 ? 2048 : places, by_places = pieces / std::max<int64_t>(tiles, 1), by_keys = ceil_div64(Sk, uneven ? 256 : 128);
     return (int)std::max<int64_t>(1, std::min(by_places, by_keys));
 }
+// Forward, bfloat16, equal tiles of many rows: one piece per compute unit.  A second one there hides less than its rows cost on their way to the merge
+// (2 x 1024 tokens, 16 heads on 4: 53 us, now 38; 700 x 12: 34 and 29; 3000 x 1: 35 and 28; 1664 x 12: 49 and 50); with ranges it
+// shortens the longest piece (1664 x 12, causal: 46 us, 53 with one).
+int64_t forward_places(bool few, bool ranges, bool f32) { return few || ranges || f32 ? 512 : 256; }
 // Row splits of the dK/dV kernel, the same with at least 256 rows each.
 int row_splits_for(int64_t tiles, int64_t M, bool uneven) {
     const int64_t pieces = uneven && tiles <= 640 ? 2048 : 512;
@@ -270,7 +274,7 @@ struct Sizes {
 };
 // false: not a supported geometry
 // uneven: float32 with key ranges
-bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool uneven, Sizes& z) {
+bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool ranges, bool f32, Sizes& z) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv || (D != 64 && D != 128)) return false;
     z.G = Hq / Hkv;
     if (Sq >= (1 << 24) || Sk >= (1 << 24) || Sq * z.G >= (1 << 24)) return false;
@@ -282,8 +286,9 @@ bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool uneven
     z.chunks = BH * ceil_div64(z.M, 32);
     if (z.q_tiles > (1 << 22) || z.k_tiles > (1 << 22) || z.chunks > (1 << 24)) return false;
     const bool few = z.M <= DENSE_FEW_ROWS;    // (single queries: bytes are what counts, and a piece's share of them is even enough)
-    z.splits = splits_for(z.q_tiles, Sk, uneven && !few);
-    z.dq_splits = splits_for(BH * ceil_div64(z.M, DENSE_TILE_ROWS), Sk, uneven);
+    const bool uneven = ranges && f32;
+    z.splits = splits_for(z.q_tiles, Sk, uneven && !few, forward_places(few, ranges, f32));
+    z.dq_splits = splits_for(BH * ceil_div64(z.M, DENSE_TILE_ROWS), Sk, uneven, 512);
     z.row_splits = row_splits_for(z.k_tiles, z.M, uneven);
     size_t off = 0;
     auto take = [&](int64_t bytes) {
@@ -319,7 +324,7 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
     if (how->q_first < INT32_MIN || how->q_first + Sq > INT32_MAX) return VMOBA_ERR_INVALID_ARG;
     if (K->dtype != Q->dtype || V->dtype != Q->dtype || O->dtype != Q->dtype) return VMOBA_ERR_UNSUPPORTED;
     if (how->cap > (Q->dtype == VMOBA_BF16 ? 4096.f : 1e30f)) return VMOBA_ERR_UNSUPPORTED;
-    if (!sizes_of(B, Hq, Hkv, Sq, Sk, D, how->key_lo != nullptr && Q->dtype == VMOBA_F32, z)) return VMOBA_ERR_UNSUPPORTED;
+    if (!sizes_of(B, Hq, Hkv, Sq, Sk, D, how->key_lo != nullptr, Q->dtype == VMOBA_F32, z)) return VMOBA_ERR_UNSUPPORTED;
     if (!reach_ok(K, Sk) || !reach_ok(V, Sk)) return VMOBA_ERR_UNSUPPORTED;
     a.Q = make_view(Q);
     a.K = make_view(K);
@@ -356,7 +361,9 @@ int check(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_ten
 
 extern "C" size_t vmoba_dense_workspace_bytes(int op, int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, int dtype) {
     Sizes y, z;      // whether there are key ranges is not known here
-    if ((dtype != VMOBA_F32 && dtype != VMOBA_BF16) || !sizes_of(B, Hq, Hkv, Sq, Sk, D, false, y) || !sizes_of(B, Hq, Hkv, Sq, Sk, D, dtype == VMOBA_F32, z)) return 0;
+    if ((dtype != VMOBA_F32 && dtype != VMOBA_BF16) || !sizes_of(B, Hq, Hkv, Sq, Sk, D, false, dtype == VMOBA_F32, y) ||
+        !sizes_of(B, Hq, Hkv, Sq, Sk, D, true, dtype == VMOBA_F32, z))
+        return 0;
     return op == VMOBA_OP_ATTN_FWD ? std::max(y.fwd, z.fwd) : op == VMOBA_OP_ATTN_BWD ? std::max(y.bwd, z.bwd) : 0;
 }
 
