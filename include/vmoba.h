@@ -379,7 +379,9 @@ size_t vmoba_dense_workspace_bytes(int op, int B, int Hq, int Hkv, int64_t Sq, i
  *  Sq, Sk from 1 on (one query against a long cache is split over its keys); Sq * Hq / Hkv and Sk below 2^24.
  *  Rows outside a query's range never reach its results, whatever they hold (NaN and infinities included).
  *  Sums and the soft-max are float32; bfloat16 inputs are multiplied on the matrix cores, weights rounded to bfloat16 for the second
- *  product; float32 inputs are multiplied in float32.
+ *  product; float32 inputs are multiplied in float32 or, in calls of many pairs, as three bfloat16 terms each, to the same precision.  (Such a call takes the
+ *  float32 instruction after all where an input, in a masked place or not, is a NaN, an infinity, larger than 2^26 or smaller than 2^-100 and not 0: the last bits
+ *  of the other rows' results may then differ, within the rounding of float32 sums.)
  *  Limit: a row stride of K and V of at least 0 and below 2^23 bytes, and Sk rows of it below 4 GiB; otherwise VMOBA_ERR_UNSUPPORTED.
  */
 int vmoba_dense_fwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, const vmoba_tensor* Q, const vmoba_tensor* K,

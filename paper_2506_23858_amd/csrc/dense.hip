@@ -244,26 +244,29 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     }
 }
 
-// Splits of a row tile's keys: as many pieces as run at a time (two per compute unit), at least 128 keys each; one query of 16 heads on 4 key
-// heads, 8 sequences of 32 760 keys: 32 tiles on 512 places.  With ranges tiles cost different amounts, and the longest of a few that all
-// run at once decides: for float32 four times as many pieces, at least 256 keys each, unless there are so many tiles that their order evens them out (2 x 2001 tokens, 16 heads on
-// 4, 64 channels, causal, forward and backward: 1450 -> 900 us).  bfloat16 keeps to one round: its groups of keys take a quarter of the time, and pieces' ends
+// Splits of a row tile's keys and, dK/dV, of a key tile's rows: as many pieces as run at a time (two per compute unit), of at least 128 keys or 256 rows each;
+// one query of 16 heads on 4 key heads, 8 sequences of 32 760 keys: 32 tiles on 512 places.  With ranges tiles cost different amounts, and
+// the longest of a few that all run at once decides: for float32 four times as many pieces (backward with split operands twice as many), of at least 256 keys each, unless there are so many tiles that
+// their order evens them out (2 x 2001 tokens, 16 heads on 4, 64 channels, causal, on the float32 instruction, forward and backward: 1450 -> 900 us; with split operands
+// forward 183 -> 149, backward 499 -> 446, 468 with four times as many).  bfloat16 keeps to one round: its groups of keys take a quarter of the time, and pieces' ends
 // cost as much (1637 tokens x 12 heads, causal: 49 us, 74 with four times the pieces).
-int splits_for(int64_t tiles, int64_t Sk, bool uneven, int64_t places) {
-    const int64_t pieces = uneven && tiles <= 640 ? 2048 : places, by_places = pieces / std::max<int64_t>(tiles, 1), by_keys = ceil_div64(Sk, uneven ? 256 : 128);
-    return (int)std::max<int64_t>(1, std::min(by_places, by_keys));
-}
+constexpr int64_t PLACES = 512, MANY_TILES = 640;
+int splits_for(int64_t tiles, int64_t pieces, int64_t most) { return (int)std::max<int64_t>(1, std::min(pieces / std::max<int64_t>(tiles, 1), most)); }
 // Forward, bfloat16, equal tiles of many rows: one piece per compute unit.  A second one there hides less than its rows cost on their way to the merge
 // (2 x 1024 tokens, 16 heads on 4: 53 us, now 38; 700 x 12: 34 and 29; 3000 x 1: 35 and 28; 1664 x 12: 49 and 50); with ranges it
 // shortens the longest piece (1664 x 12, causal: 46 us, 53 with one).
-int64_t forward_places(bool few, bool ranges, bool f32) { return few || ranges || f32 ? 512 : 256; }
-// Row splits of the dK/dV kernel, the same with at least 256 rows each.
-int row_splits_for(int64_t tiles, int64_t M, bool uneven) {
-    const int64_t pieces = uneven && tiles <= 640 ? 2048 : 512;
-    return (int)std::max<int64_t>(1, std::min(pieces / std::max<int64_t>(tiles, 1), M / 256));
-}
+int64_t forward_places(bool ranges, bool f32) { return ranges || f32 ? PLACES : PLACES / 2; }
 // More pieces of work than run at a time: their order matters.
-bool order_matters(int64_t pieces) { return pieces > 512; }
+bool order_matters(int64_t pieces) { return pieces > PLACES; }
+
+// float32 calls with enough work -- multiply-adds of one product over all pairs, masked ones too: the host does not know the ranges -- split their operands
+// (dense_split.hip).  What that costs is two launches and a pass over the inputs in either direction, and the launches of the kernels that take over where three terms
+// do not hold an input.  Without / with it, forward and backward, us, 12 heads: 512 tokens x 64 (2.0e8) 24 + 87 / 29 + 74; 512 x 128 (4.0e8) 39 + 151 / 39 + 103; 700 x 64 (3.8e8)
+// 40 + 131 / 39 + 101; 1024 x 128 88 + 330 / 66 + 218; 8 heads, 8192 x 128: 2278 + 8725 / 1312 + 4495.
+bool use_split(int64_t BH, int64_t M, int64_t Sk, int D) {
+    return M > DENSE_FEW_ROWS && (double)BH * (double)M * (double)Sk * D >= 3e8 && (uint64_t)std::max(M, Sk) * 12 * D < ((uint64_t)1 << 32) &&
+           BH * std::max(M, Sk) < ((int64_t)1 << 31);
+}
 
 struct Sizes {
     int G, rows_per_tile;
@@ -271,9 +274,10 @@ struct Sizes {
     int64_t M, q_tiles, k_tiles, chunks;       // tiles and chunks of all batch elements and key heads
     size_t part_lse, part_o, order, fwd;       // forward workspace: offsets, bytes
     size_t info, bounds, order_b, part_b, bwd; // backward
+    bool split;                                // operands of float32 calls are split: planes of Q (and dO), of K and V, and the flag
+    size_t flag, split_q, split_kv, flag_b, split_qd, split_kv_b;
 };
 // false: not a supported geometry
-// uneven: float32 with key ranges
 bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool ranges, bool f32, Sizes& z) {
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv || (D != 64 && D != 128)) return false;
     z.G = Hq / Hkv;
@@ -286,10 +290,14 @@ bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool ranges
     z.chunks = BH * ceil_div64(z.M, 32);
     if (z.q_tiles > (1 << 22) || z.k_tiles > (1 << 22) || z.chunks > (1 << 24)) return false;
     const bool few = z.M <= DENSE_FEW_ROWS;    // (single queries: bytes are what counts, and a piece's share of them is even enough)
+    z.split = f32 && use_split(BH, z.M, Sk, D);
     const bool uneven = ranges && f32;
-    z.splits = splits_for(z.q_tiles, Sk, uneven && !few, forward_places(few, ranges, f32));
-    z.dq_splits = splits_for(BH * ceil_div64(z.M, DENSE_TILE_ROWS), Sk, uneven, 512);
-    z.row_splits = row_splits_for(z.k_tiles, z.M, uneven);
+    auto pieces = [&](int64_t tiles, int64_t equal, int64_t unequal) { return uneven && tiles <= MANY_TILES ? unequal : equal; };
+    const int64_t dq_tiles = BH * ceil_div64(z.M, DENSE_TILE_ROWS), backward = (z.split ? 2 : 4) * PLACES;
+    z.splits = few ? splits_for(z.q_tiles, PLACES, ceil_div64(Sk, 128))
+                   : splits_for(z.q_tiles, pieces(z.q_tiles, forward_places(ranges, f32), 4 * PLACES), ceil_div64(Sk, uneven ? 256 : 128));
+    z.dq_splits = splits_for(dq_tiles, pieces(dq_tiles, PLACES, backward), ceil_div64(Sk, uneven ? 256 : 128));
+    z.row_splits = splits_for(z.k_tiles, pieces(z.k_tiles, PLACES, backward), z.M / 256);
     size_t off = 0;
     auto take = [&](int64_t bytes) {
         const size_t at = off;
@@ -299,12 +307,18 @@ bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool ranges
     z.part_lse = take(z.splits > 1 ? z.splits * BH * z.M * 4 : 0);
     z.part_o = take(z.splits > 1 ? z.splits * BH * z.M * D * 4 : 0);
     z.order = take(order_matters(z.q_tiles * z.splits) ? 2 * (z.q_tiles / Hkv) * 4 : 0);
+    z.flag = take(z.split ? 4 : 0);
+    z.split_q = take(z.split ? BH * z.M * 6 * D : 0);
+    z.split_kv = take(z.split ? BH * Sk * 12 * D : 0);
     z.fwd = std::max<size_t>(off, 256);
     off = 0;
     z.info = take(z.chunks * (int64_t)sizeof(RowInfo));
     z.bounds = take(z.chunks * (int64_t)sizeof(int4));
     z.order_b = take(2 * (B * ceil_div64(z.M, DENSE_TILE_ROWS) + z.k_tiles / Hkv) * 4);
     z.part_b = take(std::max<int64_t>(z.row_splits > 1 ? 2 * z.row_splits * BH * Sk : 0, z.dq_splits > 1 ? z.dq_splits * BH * z.M : 0) * D * 4);
+    z.flag_b = take(z.split ? 4 : 0);
+    z.split_qd = take(z.split ? BH * z.M * 12 * D : 0);
+    z.split_kv_b = take(z.split ? BH * Sk * 12 * D : 0);
     z.bwd = off;
     return true;
 }
@@ -400,7 +414,16 @@ extern "C" int vmoba_dense_fwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
         a.order_q = order;
     }
     if (bf16) launch_dense_fwd_bf16(D, cap, st, a);
-    else launch_dense_fwd_f32(D, cap, st, a);
+    else {
+        if (z.split) {
+            const SplitOperands x = {ws + z.split_q, ws + z.split_kv, (const int*)(ws + z.flag)};
+            launch_dense_split(D, false, st, a, x);
+            launch_dense_fwd_split(D, cap, st, a, x);
+            VMOBA_CHECK_LAUNCH();
+            a.run_if = x.flag;
+        }
+        launch_dense_fwd_f32(D, cap, st, a);
+    }
     VMOBA_CHECK_LAUNCH();
     if (a.splits > 1) {
         const dim3 grid((unsigned)ceil_div64((int64_t)B * Hkv * z.M * (D / 4), 256));
@@ -453,6 +476,13 @@ extern "C" int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
         a.order_k = order + 2 * nq;
     }
     a.splits = z.dq_splits;
+    const SplitOperands x = {ws + z.split_qd, ws + z.split_kv_b, (const int*)(ws + z.flag_b)};
+    if (z.split) {
+        launch_dense_split(D, true, st, a, x);
+        launch_dense_dq_split(D, cap, st, a, x);
+        VMOBA_CHECK_LAUNCH();
+        a.run_if = x.flag;
+    }
     if (bf16) launch_dense_dq_bf16(D, cap, st, a);
     else launch_dense_dq_f32(D, cap, st, a);
     VMOBA_CHECK_LAUNCH();
@@ -467,6 +497,7 @@ extern "C" int vmoba_dense_bwd(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, i
     } while (0)
     if (a.splits > 1) SUM(true, (int64_t)B * Hkv * z.M);
     a.splits = z.row_splits;
+    if (z.split) launch_dense_dkv_split(D, cap, st, a, x);
     if (bf16) launch_dense_dkv_bf16(D, cap, st, a);
     else launch_dense_dkv_f32(D, cap, st, a);
     VMOBA_CHECK_LAUNCH();

@@ -19,6 +19,7 @@ struct DenseArgs {
     const int *key_lo, *key_hi, *q_pos;
     long long q_first;
     float* LSE;
+    const int* run_if;             // float32 kernels: null, or a flag on the device without which they leave at once
     float *part_o, *part_lse;      // more than one split: forward [splits][B * Hkv][M][D] and [splits][B * Hkv][M] (base 2); dQ [splits][B * Hkv][M][D];
                                    // dK and dV [splits][2][B * Hkv][Sk][D]
     const int *order_q, *order_k;  // places by falling cost: [B * row tiles] and, backward, [B * key tiles]; null: as they come
@@ -239,3 +240,10 @@ void launch_dense_dq_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a);
 void launch_dense_dq_f32(int D, bool cap, hipStream_t st, const DenseArgs& a);
 void launch_dense_dkv_bf16(int D, bool cap, hipStream_t st, const DenseArgs& a);
 void launch_dense_dkv_f32(int D, bool cap, hipStream_t st, const DenseArgs& a);
+// The same from operands split into bfloat16 terms (dense_split.hip): rows of planes [B * Hkv][M][Q's three, backward dO's three][D] and
+// [B * Hkv][Sk][K's three, V's three][D]; flag: set where three terms do not hold an input, and then the kernels leave at once.
+struct SplitOperands { const char *q, *kv; const int* flag; };
+void launch_dense_split(int D, bool backward, hipStream_t st, const DenseArgs& a, const SplitOperands& x);
+void launch_dense_fwd_split(int D, bool cap, hipStream_t st, const DenseArgs& a, const SplitOperands& x);
+void launch_dense_dq_split(int D, bool cap, hipStream_t st, const DenseArgs& a, const SplitOperands& x);
+void launch_dense_dkv_split(int D, bool cap, hipStream_t st, const DenseArgs& a, const SplitOperands& x);

@@ -1,4 +1,4 @@
-// Dense attention, float32: the same decomposition as the bfloat16 kernels on v_mfma_f32_32x32x2_f32, products in full float32.
+// Dense attention, float32, for small calls and for inputs that dense_split.hip cannot split: the same decomposition as the bfloat16 kernels on v_mfma_f32_32x32x2_f32.
 //
 // Operand plumbing (lane = 32 * hf + l32): A: row l32, k = hf; B: column l32, k = hf; C/D: column l32, rows 8 * i + 4 * hf + r as value
 // 4 * i + r.  The order of a contraction is free, so
@@ -7,10 +7,7 @@
 //     column of the tile, 32 consecutive floats of two rows.
 // Tiles of 32 rows go through registers to LDS, requested one tile ahead, in rows padded by 16 bytes and in two buffers, so that a tile is one barrier.  One such instruction is 64 cycles of the
 // matrix pipe for one LDS read of 4 or a quarter of one of 16 bytes: the pipe is what bounds these kernels.
-#include "dense_common.h"
-
-#include <cfloat>
-#include <cmath>
+#include "dense_f32.h"
 
 namespace {
 
@@ -75,67 +72,12 @@ __device__ __forceinline__ void load_fragment(float (&f)[D / 2], const char* row
         for (int j = 0; j < 4; ++j) f[t + j] = x[j];
     }
 }
-// A wavefront's 32 x D result from accumulators (column l32 = row of the result) to rows: 16-byte stores.
-template <int D>
-__device__ __forceinline__ void store_row(char* row, const f32x16_t (&acc)[D / 32], float f, int hf) {
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4_t x = {acc[dt][4 * i] * f, acc[dt][4 * i + 1] * f, acc[dt][4 * i + 2] * f, acc[dt][4 * i + 3] * f};
-            *reinterpret_cast<f32x4_t*>(row + (32 * dt + 8 * i + 4 * hf) * 4) = x;
-        }
-}
-// Base-2 score of x = <q, k> before the bias (scl: signed scale * log2 e); t: tanh of the capped score.
-template <bool CAP>
-__device__ __forceinline__ float score32(const DenseArgs& a, float x, float scl, float& t) {
-    if constexpr (CAP) {
-        t = tanhf((a.negate ? -x : x) * a.cap_arg);
-        return a.cap2 * t;
-    } else {
-        return x * scl;
-    }
-}
-const f32x16_t zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-
-struct Keys { int any_lo, any_hi, all_lo, all_hi; };
-// Keys that any row of the workgroup reads, and that all rows of the wavefront read (no row without keys among them); w: 2 * NW words of LDS.
-template <int NW>
-__device__ __forceinline__ Keys tile_keys(int lo, int hi, int wave, int lane, int* w) {
-    const bool some = lo < hi;
-    Keys k = {some ? lo : INT32_MAX, some ? hi : 0, some ? lo : INT32_MAX, some ? hi : 0};
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) {
-        k.any_lo = min(k.any_lo, __shfl_xor(k.any_lo, o, 64));
-        k.any_hi = max(k.any_hi, __shfl_xor(k.any_hi, o, 64));
-        k.all_lo = max(k.all_lo, __shfl_xor(k.all_lo, o, 64));
-        k.all_hi = min(k.all_hi, __shfl_xor(k.all_hi, o, 64));
-    }
-    if constexpr (NW > 1) {
-        if (lane == 0) {
-            w[wave] = k.any_lo;
-            w[NW + wave] = k.any_hi;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            k.any_lo = min(k.any_lo, w[i]);
-            k.any_hi = max(k.any_hi, w[NW + i]);
-        }
-    }
-    k.any_lo = __builtin_amdgcn_readfirstlane(k.any_lo);
-    k.any_hi = __builtin_amdgcn_readfirstlane(k.any_hi);
-    k.all_lo = __builtin_amdgcn_readfirstlane(k.all_lo);
-    k.all_hi = __builtin_amdgcn_readfirstlane(k.all_hi);
-    if (k.any_lo >= k.any_hi) k.any_lo = k.any_hi = 0;
-    return k;
-}
-
 template <int D, int NW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) {
     constexpr int NT = 64 * NW, TILE = 32 * PITCH<D>;
     __shared__ __align__(16) float smem[2][2 * TILE];
     __shared__ int words[2 * NW];
+    if (a.run_if && !*a.run_if) return;
     const int tiles = (a.M + 32 * NW - 1) / (32 * NW);
     const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
     if (piece.rank < 0) return;
@@ -155,7 +97,7 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
     load_fragment<D>(qf, row_ptr(a.Q, b, q, h, 4), hf);
     f32x16_t acc[D / 32];
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16;
+    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zeros16();
     const float none = CAP || BIAS || scl > 0.f ? -INFINITY : INFINITY;      // stands for a masked score
     float m_run = -3e38f, l_run = 0.f;
     bool found = false;                                      // values of V that over_rows took out
@@ -180,7 +122,7 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
         const float* tk = smem[buf];
         if (kb + 32 < k_end) fetch(kb + 32);
         const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi || kb + 32 > k_end;
-        f32x16_t s = over_channels<D>(tk, qf, zero16, l32, hf);
+        f32x16_t s = over_channels<D>(tk, qf, zeros16(), l32, hf);
         const float rel = BIAS ? (float)(pos - kb - 4 * hf) : 0.f;
         const int first_key = lo - kb - 4 * hf, end = min(hi, k_end) - kb - 4 * hf;
         float mx = -INFINITY;
@@ -244,20 +186,12 @@ __global__ __launch_bounds__(64 * NW, 1) void dense_fwd_f32_kernel(DenseArgs a) 
                                       __shfl(hi, 16 + (lane & 15), 64), lse2, __shfl(lse2, 16 + (lane & 15), 64));
 }
 
-// P and dz of one pair from x = <q, k> and dp = dP - delta.
-template <bool CAP>
-__device__ __forceinline__ void pair_gradient(const DenseArgs& a, float x, float scl, float bias2, float c2, float dp, float& p, float& dz) {
-    float t = 0.f;
-    const float s2 = score32<CAP>(a, x, scl, t);
-    p = exp2_raw(CAP ? s2 - bias2 + c2 : fmaf(x, scl, c2 - bias2));
-    dz = p * dp * (CAP ? 1.f - t * t : 1.f);
-}
-
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     constexpr int TILE = 32 * PITCH<D>;
     __shared__ __align__(16) float smem[2][2 * TILE];
     __shared__ int words[8];
+    if (a.run_if && !*a.run_if) return;
     const int tiles = (a.M + 127) / 128;
     const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
     if (piece.rank < 0) return;
@@ -278,7 +212,7 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
     load_fragment<D>(dof, row_ptr(a.dO, b, q, h, 4), hf);
     f32x16_t acc[D / 32];
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16;
+    for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zeros16();
     const char *kbase = row_ptr(a.K, b, 0, hk, 4), *vbase = row_ptr(a.V, b, 0, hk, 4);
     const long long kss = a.K.stride_s * 4, vss = a.V.stride_s * 4;
     Stage<D, 256> sk, sv;
@@ -300,7 +234,7 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
         const float* tk = smem[buf];
         if (kb + 32 < k_end) fetch(kb + 32);
         const bool masked = kb < keys.all_lo || kb + 32 > keys.all_hi || kb + 32 > k_end;
-        f32x16_t s = over_channels<D>(tk, qf, zero16, l32, hf), dp;
+        f32x16_t s = over_channels<D>(tk, qf, zeros16(), l32, hf), dp;
 #pragma unroll
         for (int v = 0; v < 16; ++v) dp[v] = nd;
         dp = over_channels<D>(tk + TILE, dof, dp, l32, hf);
@@ -309,9 +243,9 @@ __global__ __launch_bounds__(256, 1) void dense_dq_f32_kernel(DenseArgs a) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int key = 8 * (v >> 2) + (v & 3);
-            float p, dz;
-            pair_gradient<CAP>(a, s[v], scl, BIAS ? slope2 * fabsf(rel - (float)key) : 0.f, c2, dp[v], p, dz);
-            s[v] = dz;
+            float f;
+            const float p = weight32<CAP>(a, s[v], scl, BIAS ? c2 - slope2 * fabsf(rel - (float)key) : c2, f);
+            s[v] = p * dp[v] * f;
         }
         if (masked) {
 #pragma unroll
@@ -333,6 +267,7 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
     constexpr int TILE = 32 * PITCH<D>;
     __shared__ __align__(16) float smem[2][2 * TILE];
     __shared__ RowInfo infos[2];
+    if (a.run_if && !*a.run_if) return;
     const int tiles = (a.Sk + 127) / 128;
     const DensePiece piece = dense_piece(a.B * tiles * a.splits, a.Hkv);
     if (piece.rank < 0) return;
@@ -349,7 +284,7 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
     load_fragment<D>(vf, row_ptr(a.V, b, min(key, a.Sk - 1), hk, 4), hf);
     f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zero16;
+    for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zeros16();
     Stage<D, 256> sq, so;
     uint32_t si = 0;                                         // the thread's word of the row information
     ChunkWalk walk(bounds, n_chunks, k0, k0 + 128, lane, task.split, a.splits);
@@ -382,17 +317,16 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
         c = walk.next();
         if (c >= 0) fetch(c);
         const bool masked = kw < all_lo || kw + 32 > all_hi;
-        f32x16_t s = over_channels<D>(tq, kf, zero16, l32, hf), dp;
+        f32x16_t s = over_channels<D>(tq, kf, zeros16(), l32, hf), dp;
 #pragma unroll
         for (int v = 0; v < 16; ++v) dp[v] = ri.ndelta[8 * (v >> 2) + 4 * hf + (v & 3)];
         dp = over_channels<D>(tq + TILE, vf, dp, l32, hf);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int r = 8 * (v >> 2) + 4 * hf + (v & 3);
-            float p, dz;
-            pair_gradient<CAP>(a, s[v], scl, BIAS ? ri.slope2[r] * fabsf((float)(ri.pos[r] - key)) : 0.f, ri.c2[r], dp[v], p, dz);
-            s[v] = p;
-            dp[v] = dz;
+            float f;
+            s[v] = weight32<CAP>(a, s[v], scl, BIAS ? ri.c2[r] - ri.slope2[r] * fabsf((float)(ri.pos[r] - key)) : ri.c2[r], f);
+            dp[v] *= s[v] * f;
         }
         if (masked) {
 #pragma unroll
@@ -417,14 +351,6 @@ __global__ __launch_bounds__(256, 1) void dense_dkv_f32_kernel(DenseArgs a) {
         store_row<D>(const_cast<char*>(row_ptr(a.dV, b, key, hk, 4)), dv, 1.f, hf);
     }
 }
-
-#define BY_SCORES(LAUNCH)                   \
-    do {                                    \
-        if (cap && a.slopes) LAUNCH(true, true);   \
-        else if (cap) LAUNCH(true, false);         \
-        else if (a.slopes) LAUNCH(false, true);    \
-        else LAUNCH(false, false);                 \
-    } while (0)
 
 template <int D, int NW>
 void launch_fwd(bool cap, hipStream_t st, const DenseArgs& a) {

@@ -427,6 +427,70 @@ def test_dense_cache_beyond_32_bit_offsets():
     assert bool((got["O"][:2] == 0).all())
 
 
+# float32 calls of 3e8 multiply-adds and more multiply operands split into bfloat16 terms.  The bound of a product holds for them, too: a term left out is below
+# 2^-25 of it, and its sum is rounded once per matrix instruction, 6 times in 16 channels, where the bound counts every channel.
+MANY = [(64, 1, 6, 2, 901, 901), (128, 2, 3, 3, 641, 641), (128, 1, 5, 1, 333, 1511), (64, 3, 4, 4, 700, 613)]
+
+
+@pytest.mark.parametrize("D,B,Hq,Hkv,Sq,Sk", MANY)
+@pytest.mark.parametrize("mask,cap,bias,scale", [("none", 0.0, False, None), ("none", 7.0, True, -0.1), ("causal", 0.0, True, None), ("docs", 9.0, False, None), ("any", 0.0, False, -0.2)])
+def test_dense_float32_calls_of_many_pairs(D, B, Hq, Hkv, Sq, Sk, mask, cap, bias, scale):
+    Q, K, V, dO = tensors(B, Hq, Hkv, Sq, Sk, D, F32)
+    lo = hi = None
+    if mask != "none":
+        lo, hi = (torch.empty(B, Sq, dtype=torch.int32, device="cuda") for _ in range(2))
+    if mask == "any":      # empty ones, reversed ones, beyond both ends
+        g = torch.Generator().manual_seed(6)
+        lo.copy_(torch.randint(-50, Sk, (B, Sq), generator=g))
+        hi.copy_(lo.cpu() + torch.randint(-30, Sk, (B, Sq), generator=g))
+    elif mask != "none":
+        docs = dict(doc_off=int32([[0, 65, 65, 301, Sk - 120]]), prefix=int32([[10, 0, 100, 7]])) if mask == "docs" else {}
+        vb.vmoba_key_ranges(B, Sq, Sk, lo, hi, causal=True, q_first=Sk - Sq, **docs)
+    check(Q, K, V, dO, lo, hi, scale=scale, cap=cap, slopes=torch.linspace(0.001, 0.05, Hq, device="cuda") if bias else None, q_first=Sk - Sq)
+
+
+@pytest.mark.parametrize("where", ["masked NaN", "masked infinity", "large", "small"])
+def test_dense_float32_values_that_terms_do_not_hold(where):
+    """Such a call gives what the float32 instruction gives, and the next one, in the same workspace or a replay of the same graph, split operands again."""
+    B, H, S, D, end = 1, 6, 901, 64, 850
+    Q, K, V, dO = (t.clone() for t in tensors(B, H, H, S, S, D, F32))
+    lo, hi = (torch.empty(B, S, dtype=torch.int32, device="cuda") for _ in range(2))
+    vb.vmoba_key_ranges(B, S, S, lo, hi, doc_off=int32([[0, end]]), causal=True)
+    for t in (Q, K, V, dO):
+        t[:, end:] = 0.0
+    plain = [t.clone() for t in (Q, K, V, dO)]
+    clean = check(Q, K, V, dO, lo, hi)
+    if "masked" in where:
+        for t in (Q, K, V, dO):
+            t[:, end:] = math.nan if "NaN" in where else -math.inf
+    else:      # values that are read: scores stay moderate
+        V[0, 3, 0, 5], dO[0, 700, 1, 2] = (3e9, -2e8) if where == "large" else (1e-36, -1e-33)
+    other = check(Q, K, V, dO, lo, hi)
+    if "masked" in where:      # off by the rounding of the sums alone, and nothing where there is nothing
+        assert all(bool((other[n][:, end:] == 0).all()) for n in ("O", "dQ", "dK", "dV"))
+    # a graph whose inputs change between such values and others
+    size, ws = (B, H, H, S, S, D), torch.empty(max(vb.vmoba_dense_workspace_bytes(op, B, H, H, S, S, D, vb.VMOBA_F32) for op in (vb.OP_ATTN_FWD, vb.OP_ATTN_BWD)),
+                                               dtype=torch.uint8, device="cuda")
+    ins, odd = [t.clone() for t in plain], [t.clone() for t in (Q, K, V, dO)]
+    out = {n: torch.empty_like(t) for n, t in clean.items()}
+    how = dict(softmax_scale=1 / math.sqrt(D), key_lo=lo, key_hi=hi)
+
+    def step():
+        vb.vmoba_dense_fwd(*size, *ins[:3], out["O"], out["LSE"], ws, **how)
+        vb.vmoba_dense_bwd(*size, *ins[:3], out["O"], out["LSE"], ins[3], out["dQ"], out["dK"], out["dV"], ws, **how)
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for values, want in ((odd, other), (plain, clean), (odd, other), (plain, clean)):
+        for t, v in zip(ins, values):
+            t.copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in out:
+            assert torch.equal(out[n].view(torch.int32), want[n].view(torch.int32)), n
+
+
 # ---------------------------------------------------------------------------------------------------------------- together
 def layer_reference(Q, K, V, wq, wk, dims, grid, norm, dO, cap):
     """Norm, rotation, dense attention in 64 bits, and their gradients by automatic differentiation."""
