@@ -244,9 +244,10 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     }
 }
 
-// Splits of a row tile's keys and, dK/dV, of a key tile's rows: as many pieces as run at a time (two per compute unit), of at least 128 keys or 256 rows each;
-// one query of 16 heads on 4 key heads, 8 sequences of 32 760 keys: 32 tiles on 512 places.  With ranges tiles cost different amounts, and
-// the longest of a few that all run at once decides: for float32 four times as many pieces (backward with split operands twice as many), of at least 256 keys each, unless there are so many tiles that
+// Splits of a row tile's keys and, dK/dV, of a key tile's rows: as many pieces as run at a time (two per compute unit), of at least 256 keys or rows each; float32 without
+// ranges, whose keys take four times as long, and single queries (one of 16 heads on 4 key heads, 8 sequences of 32 760 keys: 32 tiles on 512 places): 128.  (bfloat16 with 128:
+// 256 tokens x 12 heads 19 us, 17 with 256; 600 x 12, causal, 32 and 29; 512 x 12 alike; 512 x 2 18 and 20.)  With ranges tiles cost different amounts, and
+// the longest of a few that all run at once decides: for float32 four times as many pieces (backward with split operands twice as many), unless there are so many tiles that
 // their order evens them out (2 x 2001 tokens, 16 heads on 4, 64 channels, causal, on the float32 instruction, forward and backward: 1450 -> 900 us; with split operands
 // forward 183 -> 149, backward 499 -> 446, 468 with four times as many).  bfloat16 keeps to one round: its groups of keys take a quarter of the time, and pieces' ends
 // cost as much (1637 tokens x 12 heads, causal: 49 us, 74 with four times the pieces).
@@ -293,10 +294,11 @@ bool sizes_of(int B, int Hq, int Hkv, int64_t Sq, int64_t Sk, int D, bool ranges
     z.split = f32 && use_split(BH, z.M, Sk, D);
     const bool uneven = ranges && f32;
     auto pieces = [&](int64_t tiles, int64_t equal, int64_t unequal) { return uneven && tiles <= MANY_TILES ? unequal : equal; };
+    const int64_t least = f32 && !ranges ? 128 : 256;
     const int64_t dq_tiles = BH * ceil_div64(z.M, DENSE_TILE_ROWS), backward = (z.split ? 2 : 4) * PLACES;
     z.splits = few ? splits_for(z.q_tiles, PLACES, ceil_div64(Sk, 128))
-                   : splits_for(z.q_tiles, pieces(z.q_tiles, forward_places(ranges, f32), 4 * PLACES), ceil_div64(Sk, uneven ? 256 : 128));
-    z.dq_splits = splits_for(dq_tiles, pieces(dq_tiles, PLACES, backward), ceil_div64(Sk, uneven ? 256 : 128));
+                   : splits_for(z.q_tiles, pieces(z.q_tiles, forward_places(ranges, f32), 4 * PLACES), ceil_div64(Sk, least));
+    z.dq_splits = splits_for(dq_tiles, pieces(dq_tiles, PLACES, backward), ceil_div64(Sk, least));
     z.row_splits = splits_for(z.k_tiles, pieces(z.k_tiles, PLACES, backward), z.M / 256);
     size_t off = 0;
     auto take = [&](int64_t bytes) {
