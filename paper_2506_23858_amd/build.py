@@ -18,7 +18,7 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
 # attn_bwd: its large kernel names the matrix instructions whose sums belong in accumulator registers and interleaves matrix and
 # vector instructions one by one; results of the others go to ordinary registers, and the vectorizer, which would gather the
 # vector instructions in one place, stays off.
-# attn_split, dense_*: the same choice of registers (the largest kernels spill otherwise).
+# attn_split, dense_f32, dense_split: the same choice of registers (the largest kernels spill otherwise).
 FILE_FLAGS = {"attn_bwd.hip": ["-fno-slp-vectorize", "-mllvm", "-amdgpu-mfma-vgpr-form"],
               "attn_split.hip": ["-fno-slp-vectorize", "-mllvm", "-amdgpu-mfma-vgpr-form"],
               "dense_f32.hip": ["-fno-slp-vectorize", "-mllvm", "-amdgpu-mfma-vgpr-form"],
