@@ -263,7 +263,7 @@ bool order_matters(int64_t pieces) { return pieces > PLACES; }
 // float32 calls with enough work -- multiply-adds of one product over all pairs, masked ones too: the host does not know the ranges -- split their operands
 // (dense_split.hip).  What that costs is two launches and a pass over the inputs in either direction, and the launches of the kernels that take over where three terms
 // do not hold an input.  Without / with it, forward and backward, us, 12 heads: 512 tokens x 64 (2.0e8) 24 + 87 / 29 + 74; 512 x 128 (4.0e8) 39 + 151 / 39 + 103; 700 x 64 (3.8e8)
-// 40 + 131 / 39 + 101; 1024 x 128 88 + 330 / 66 + 218; 8 heads, 8192 x 128: 2278 + 8725 / 1312 + 4495.
+// 40 + 131 / 39 + 101; 1024 x 128 88 + 330 / 66 + 218; 8 heads, 8192 x 128: 2278 + 8725 / 1259 + 4379.
 bool use_split(int64_t BH, int64_t M, int64_t Sk, int D) {
     return M > DENSE_FEW_ROWS && (double)BH * (double)M * (double)Sk * D >= 3e8 && (uint64_t)std::max(M, Sk) * 12 * D < ((uint64_t)1 << 32) &&
            BH * std::max(M, Sk) < ((int64_t)1 << 31);

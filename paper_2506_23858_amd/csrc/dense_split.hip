@@ -9,8 +9,8 @@
 //
 // Soft-max weights and dz are split in registers after a multiplication by 2^16 (attn_split.hip), taken back where sums are written.
 //
-// 8192 tokens x 8 heads x 128, float32 instruction -> these: forward 2.28 -> 1.31 ms (209 TFLOP/s of float32 work; that instruction alone holds 153), backward 8.73 ->
-// 4.50 ms; 64 channels 1.33 -> 0.85 and 3.97 -> 2.65.  What bounds them: the matrix pipe, beside the splitting of weights, 6 vector instructions a value and term.
+// 8192 tokens x 8 heads x 128, float32 instruction -> these: forward 2.28 -> 1.26 ms (218 TFLOP/s of float32 work; that instruction alone holds 153), backward 8.73 ->
+// 4.38 ms; 64 channels 1.33 -> 0.71 and 3.97 -> 2.30.  What bounds them: the matrix pipe, beside the splitting of weights, 6 vector instructions a value and term.
 #include "dense_f32.h"
 #include "split_common.h"
 
@@ -233,7 +233,8 @@ __global__ __launch_bounds__(256, 1) void dense_dq_split_kernel(DenseArgs a, Spl
 }
 
 // dK/dV: 128 keys own (32 per wavefront), chunks of 32 packed rows walked through two buffers: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dz.
-// D = 64: two wavefronts per SIMD although 24 registers spill (2 x 2001 tokens, 16 heads on 4, causal, backward: 475 -> 446 us; 5000 x 12, causal: 868 -> 775).
+// D = 64: two wavefronts per SIMD although 24 registers spill (2 x 2001 tokens, 16 heads on 4, causal, backward: 475 -> 446 us; 5000 x 12, causal: 868 -> 775;
+// the reloads wait for the requests in flight, but requesting behind them gains nothing).
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void dense_dkv_split_kernel(DenseArgs a, SplitOperands x) {
     using ST = SplitTile<D>;
